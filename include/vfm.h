@@ -76,7 +76,9 @@ typedef enum {
   VFM_ERR_WORKSPACE = 7,   /* workspace NULL, misaligned or too small */
   VFM_ERR_LAUNCH = 8,      /* the HIP runtime refused a launch */
   VFM_ERR_ALIGN = 9,       /* a tensor pointer is not 16-byte aligned */
-  VFM_ERR_SCRATCH = 10     /* sizes beyond the built-in scratch of vfm_attn_bwd_noalloc */
+  VFM_ERR_SCRATCH = 10,    /* sizes beyond the built-in scratch of vfm_attn_bwd_noalloc */
+  VFM_ERR_STRIDE = 11,     /* a token stride that is no multiple of 8 or smaller than a token */
+  VFM_ERR_PAGE = 12        /* page_size no power of two from 16 to 2^20, or a negative number of pages */
 } vfm_status;
 
 typedef enum { VFM_BF16 = 0, VFM_F32 = 1 /* not implemented: VFM_ERR_DTYPE */ } vfm_dtype;
@@ -401,6 +403,120 @@ VFM_API int vfm_schedule_units(const int32_t* cu_seqlens, int n_seqs, int total_
  */
 VFM_API int vfm_attn_fwd_tile_rows(const int32_t* cu_seqlens, int n_seqs, int total_tokens,
                            int head_dim, int run, int* rows_per_tile);
+
+/*
+ * Causal attention with grouped heads, forward.  Sequence s owns queries
+ * [cu_seqlens_q[s], cu_seqlens_q[s+1]) and keys/values [cu_seqlens_kv[s],
+ * cu_seqlens_kv[s+1]), Lq and Lk of them; its last query sees its last key: query i
+ * (from 0) sees the keys j <= i + Lk - Lq (self-attention where the lengths
+ * are equal; a chunk of a prompt against all that came before it where Lk is
+ * greater).  n_heads is a multiple of n_kv_heads; query head h uses K/V head
+ * h / (n_heads / n_kv_heads):
+ *     S_ij  = scale * sum_d q[i,h,d] k[j,kvh,d]
+ *     out_i = sum_j softmax_j(S_ij) v[j,kvh,:],   lse_i = ln sum_j exp(S_ij)
+ * A query that sees no key (Lq > Lk) gets out 0 and lse -infinity.
+ * q: bf16 [total_q, n_heads, head_dim], k, v: bf16 [total_kv, n_kv_heads, head_dim],
+ * q_stride, k_stride, v_stride elements from one token to the next (multiples of
+ * 8; the heads of a token are contiguous), so that they may be parts of one
+ * projection's output; out: bf16 [total_q, n_heads, head_dim] and lse: fp32
+ * [n_heads, total_q], contiguous, fully overwritten.  Both cu arrays are host
+ * int32 [n_seqs+1].  One sequence's rows of a tensor span less than 4 GiB, and
+ * total_q * n_heads <= 2^27 (SHAPE).  k and v may be NULL if total_kv is 0.
+ * A query's results depend on no key that it does not see.  The result is
+ * bitwise reproducible from run to run.
+ * workspace: device, 256-byte aligned, vfm_cattn_fwd_workspace_size() bytes (0: none
+ * needed, may be NULL).
+ * Errors: NULL, SHAPE, STRIDE, CU_SEQLENS, DTYPE, ALIGN, WORKSPACE, LAUNCH.
+ */
+VFM_API size_t vfm_cattn_fwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,
+                                    int total_q, int total_kv, int n_heads, int n_kv_heads, int head_dim);
+VFM_API int vfm_cattn_fwd(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,
+                  int total_q, int total_kv, int n_heads, int n_kv_heads, int head_dim, float scale,
+                  void* out, float* lse, void* workspace, size_t workspace_bytes,
+                  vfm_dtype dt, void* hip_stream);
+
+/*
+ * Causal attention with grouped heads, backward: dq [total_q, n_heads, head_dim], dk, dv
+ * [total_kv, n_kv_heads, head_dim] from dout, given the forward's out and lse, with the
+ * formulas of vfm_attn_bwd over the pairs that are seen; dk and dv are sums over
+ * the query heads of the group.  dq of a query that sees no key and dk, dv of a
+ * key that none sees are 0.  Each has a token stride of its own (as q, k, v).
+ * All are fully overwritten and bitwise reproducible; they must not overlap the inputs.
+ * Delta of a query that sees at most 32 keys is formed as sum_j P_ij (dout_i . v_j), as in
+ * vfm_attn_bwd.  workspace: device, 256-byte aligned, vfm_cattn_bwd_workspace_size() bytes.
+ * Errors: NULL, SHAPE, STRIDE, CU_SEQLENS, DTYPE, ALIGN, WORKSPACE, LAUNCH.
+ */
+VFM_API size_t vfm_cattn_bwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,
+                                    int total_q, int total_kv, int n_heads, int n_kv_heads, int head_dim);
+VFM_API int vfm_cattn_bwd(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  const void* out, const float* lse, const void* dout,
+                  const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,
+                  int total_q, int total_kv, int n_heads, int n_kv_heads, int head_dim, float scale,
+                  void* dq, int64_t dq_stride, void* dk, int64_t dk_stride, void* dv, int64_t dv_stride,
+                  void* workspace, size_t workspace_bytes, vfm_dtype dt, void* hip_stream);
+
+/*
+ * The key/value cache in 4 bits.  It is four device buffers of the caller's:
+ *   k4, v4              uint8 [n_pages][n_kv_heads][page_size][head_dim / 2]
+ *   k_scales, v_scales  uint8 [n_pages][n_kv_heads][page_size][head_dim / 32]
+ * A row (token, K/V head) is cut into blocks of 32 consecutive elements.  An element is an
+ * E2M1 code (sign, 2 exponent bits, 1 mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6), two to a
+ * byte, element 2b in the low half of byte b; a block's scale byte x in 1..254 stands for the
+ * factor 2^(x - 127) (E8M0): value = code * factor.  vfm_kv4_append takes
+ *   e      = the largest integer with  max|x| * 2^e <= 6  over the block, limited to
+ *            [-125, 120], 0 for an all-zero block;   scale byte = 127 - e
+ *   code   = x * 2^e rounded to the nearest (ties to even, at most 6 in magnitude)
+ * A block with a NaN or an infinity gets scale byte 255 and zero codes; it reads as NaN.
+ *
+ * Pages: place p of sequence s is row p % page_size of page pages[s][p / page_size]; pages is a DEVICE
+ * int32 [n_seqs][max_pages], lens a DEVICE int32 [n_seqs]: the tokens that s held before this step.
+ * They are read by the kernels, so that a captured step serves any state.  The new tokens of a
+ * step are packed: sequence s has cu_seqlens[s+1] - cu_seqlens[s] (HOST array), at places
+ * lens[s], lens[s] + 1, ...  The same lens serves vfm_kv4_append and vfm_kv4_attn of one step; the caller
+ * adds to it afterwards.  lens[s] < 0 marks an idle slot: nothing is written for it, its out
+ * rows are 0 and its lse -infinity.  An entry of pages outside [0, n_pages) and a place past
+ * max_pages * page_size hold nothing: they are not written, not attended to, and gathered as
+ * zeros.  Pages may be shared between sequences to read; a page that a call writes to must belong
+ * to one sequence.  page_size: a power of two from 16 to 2^20.  The cache may exceed 4 GiB.
+ * n_kv_heads * total_tokens <= 2^27; of vfm_kv4_attn n_heads * total_tokens <= 2^22 (SHAPE).
+ */
+/* Quantises k, v (bf16 [total_tokens, n_kv_heads, head_dim], token strides as above) into the cache.
+ * Errors: NULL, SHAPE, STRIDE, PAGE, CU_SEQLENS, DTYPE, ALIGN, LAUNCH. */
+VFM_API int vfm_kv4_append(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                   const int32_t* cu_seqlens, int n_seqs, int total_tokens, const int32_t* lens,
+                   const int32_t* pages, int max_pages, void* k4, void* v4, void* k_scales, void* v_scales,
+                   int n_pages, int page_size, int n_kv_heads, int head_dim, vfm_dtype dt, void* hip_stream);
+
+/* Reads the places 0 .. cu_seqlens[s+1] - cu_seqlens[s] - 1 of every sequence back to bf16: k, v
+ * [total_tokens, n_kv_heads, head_dim], contiguous (what vfm_cattn_fwd takes).  The values are exact.
+ * Errors: NULL, SHAPE, PAGE, CU_SEQLENS, DTYPE, ALIGN, LAUNCH. */
+VFM_API int vfm_kv4_gather(const void* k4, const void* v4, const void* k_scales, const void* v_scales,
+                   int n_pages, int page_size, const int32_t* pages, int max_pages,
+                   const int32_t* cu_seqlens, int n_seqs, int total_tokens, int n_kv_heads, int head_dim,
+                   void* k, void* v, vfm_dtype dt, void* hip_stream);
+
+/*
+ * Attention of the new tokens over the cache, which holds their own keys and values already:
+ * new token t (from 0) of sequence s sees the places 0 .. lens[s] + t.  Formulas and head
+ * groups of vfm_cattn_fwd, with k, v the values that the cache stands for.  q: bf16 [total_tokens,
+ * n_heads, head_dim] with a token stride; out: bf16 [total_tokens, n_heads, head_dim], lse: fp32
+ * [n_heads, total_tokens], contiguous, fully overwritten.  A token that sees a block with
+ * scale byte 255 gets NaN throughout.  Meant for few new tokens per sequence (one, or a handful
+ * of drafted ones): the cache is read once per 64 rows (tokens times heads of a group); a long chunk
+ * of a prompt is better served by vfm_kv4_gather and vfm_cattn_fwd.
+ * workspace: device, 256-byte aligned, vfm_kv4_attn_workspace_size() bytes; its contents need not be
+ * initialised.  No atomics: bitwise reproducible from run to run.
+ * Errors: NULL, SHAPE, STRIDE, PAGE, CU_SEQLENS, DTYPE, ALIGN, WORKSPACE, LAUNCH.
+ */
+VFM_API size_t vfm_kv4_attn_workspace_size(const int32_t* cu_seqlens, int n_seqs, int total_tokens,
+                                   int n_heads, int n_kv_heads, int head_dim);
+VFM_API int vfm_kv4_attn(const void* q, int64_t q_stride, const void* k4, const void* v4,
+                 const void* k_scales, const void* v_scales, int n_pages, int page_size,
+                 const int32_t* pages, int max_pages, const int32_t* lens,
+                 const int32_t* cu_seqlens, int n_seqs, int total_tokens, int n_heads, int n_kv_heads,
+                 int head_dim, float scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                 vfm_dtype dt, void* hip_stream);
 
 /* Static, human-readable text for a vfm_status. */
 VFM_API const char* vfm_strerror(int status);

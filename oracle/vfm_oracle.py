@@ -539,3 +539,144 @@ def attn_bwd_cols(q, k, v, dout, cu_seqlens, scale: float, head: int, cols, row_
         dS = Pc * (dO @ Vc.T - delta)
         dk += scale * (dS.T @ Q)
     return dk, dv
+
+
+# ---------------------------------------------------------------- causal attention with grouped heads
+# Query i of a sequence sees the keys j <= i + Lk - Lq (the last query sees the last key); query head h uses
+# K/V head h // (heads / kv_heads).  A query that sees nothing has output 0 and lse -inf.
+def _causal_probs(q, k, scale: float):
+    """P and lse of one head of one sequence."""
+    lq, lk = q.shape[0], k.shape[0]
+    seen = np.arange(lk)[None, :] <= np.arange(lq)[:, None] + (lk - lq)
+    S = np.where(seen, scale * (q @ k.T), -np.inf)
+    P = np.zeros((lq, lk))
+    lse = np.full(lq, -np.inf)
+    some = seen.any(axis=1)
+    if some.any():
+        m = S[some].max(axis=1, keepdims=True)
+        e = np.exp(S[some] - m)
+        l = e.sum(axis=1, keepdims=True)
+        P[some] = e / l
+        lse[some] = (m + np.log(l))[:, 0]
+    return P, lse
+
+
+def cattn_fwd(q, k, v, cu_seqlens_q, cu_seqlens_kv, scale: float):
+    """out [total_q, heads, D], lse [heads, total_q] of causal attention with grouped heads."""
+    q, k, v = _as_f64(q), _as_f64(k), _as_f64(v)
+    cq, ck = _check_cu(cu_seqlens_q, q.shape[0]), _check_cu(cu_seqlens_kv, k.shape[0])
+    heads, group = q.shape[1], q.shape[1] // k.shape[1]
+    out = np.zeros_like(q)
+    lse = np.full((heads, q.shape[0]), -np.inf)
+    for s in range(len(cq) - 1):
+        a, b, c, d = cq[s], cq[s + 1], ck[s], ck[s + 1]
+        for h in range(heads):
+            P, lse[h, a:b] = _causal_probs(q[a:b, h], k[c:d, h // group], scale)
+            out[a:b, h] = P @ v[c:d, h // group]
+    return out, lse
+
+
+def cattn_bwd(q, k, v, dout, cu_seqlens_q, cu_seqlens_kv, scale: float):
+    """dq, dk, dv of sum(out * dout); dk, dv are sums over the query heads of a group."""
+    q, k, v, dout = _as_f64(q), _as_f64(k), _as_f64(v), _as_f64(dout)
+    cq, ck = _check_cu(cu_seqlens_q, q.shape[0]), _check_cu(cu_seqlens_kv, k.shape[0])
+    heads, group = q.shape[1], q.shape[1] // k.shape[1]
+    dq, dk, dv = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)
+    for s in range(len(cq) - 1):
+        a, b, c, d = cq[s], cq[s + 1], ck[s], ck[s + 1]
+        for h in range(heads):
+            n = h // group
+            P, _ = _causal_probs(q[a:b, h], k[c:d, n], scale)
+            dP = dout[a:b, h] @ v[c:d, n].T
+            delta = (P * dP).sum(axis=1, keepdims=True)
+            dS = P * (dP - delta)
+            dq[a:b, h] = scale * (dS @ k[c:d, n])
+            dk[c:d, n] += scale * (dS.T @ q[a:b, h])
+            dv[c:d, n] += P.T @ dout[a:b, h]
+    return dq, dk, dv
+
+
+# ---------------------------------------------------------------- the 4-bit key/value cache
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def kv4_encode(x):
+    """Codes [..., D/2] (two to a byte, the first element low) and scale bytes [..., D/32] of rows [..., D]: per block of 32
+    the largest e in [-125, 120] with max|x| 2^e <= 6, byte 127 - e, codes nearest to x 2^e (ties to the even code);
+    255 and zero codes for a block with a NaN or an infinity."""
+    x = _as_f64(x)
+    blocks = x.reshape(-1, 32)
+    codes = np.zeros(blocks.shape, dtype=np.uint8)
+    scales = np.zeros(blocks.shape[0], dtype=np.uint8)
+    for n, row in enumerate(blocks):
+        if not np.all(np.isfinite(row)):
+            scales[n] = 255
+            continue
+        top = np.abs(row).max()
+        e = 0
+        if top > 0:
+            e = 120
+            while e > -125 and top * 2.0 ** e > 6.0:
+                e -= 1
+        scales[n] = 127 - e
+        for i, y in enumerate(row * 2.0 ** e):
+            far = np.abs(E2M1 - abs(y))
+            near = np.flatnonzero(far == far.min())
+            code = next((c for c in near if c % 2 == 0), near[0])
+            codes[n, i] = code + (8 if np.signbit(y) else 0)
+    codes = codes.reshape(*x.shape[:-1], x.shape[-1] // 2, 2)
+    return codes[..., 0] | (codes[..., 1] << 4), scales.reshape(*x.shape[:-1], x.shape[-1] // 32)
+
+
+def kv4_decode(codes, scales):
+    """Values of rows [..., D/2] of codes and [..., D/32] of scale bytes."""
+    codes, scales = np.asarray(codes), np.asarray(scales)
+    c = np.stack((codes & 15, codes >> 4), axis=-1).reshape(*codes.shape[:-1], codes.shape[-1] * 2)
+    x = np.where(c >= 8, -1.0, 1.0) * E2M1[c & 7]
+    f = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return x * np.repeat(f, 32, axis=-1)
+
+
+def kv4_rows(codes, scales, pages, n: int):
+    """Places 0 .. n-1 of one sequence, [n, kv_heads, D]: codes [n_pages, kv_heads, page, D/2], pages the sequence's list.  A place
+    without a page is None in the second value (True where there is one)."""
+    n_pages, _, page, _ = codes.shape
+    D = codes.shape[-1] * 2
+    x = np.zeros((n, codes.shape[1], D))
+    there = np.zeros(n, dtype=bool)
+    for p in range(n):
+        if p // page < len(pages) and 0 <= pages[p // page] < n_pages:
+            there[p] = True
+            x[p] = kv4_decode(codes[pages[p // page], :, p % page], scales[pages[p // page], :, p % page])
+    return x, there
+
+
+def kv4_attn(q, k4, v4, ks, vs, pages, lens, cu_seqlens, scale: float):
+    """out, lse of the new tokens over the cache: token t of sequence s sees the places 0 .. lens[s] + t that hold something."""
+    q = _as_f64(q)
+    cu = _check_cu(cu_seqlens, q.shape[0])
+    heads, group = q.shape[1], q.shape[1] // k4.shape[1]
+    room = pages.shape[1] * k4.shape[2]
+    out = np.zeros_like(q)
+    lse = np.full((heads, q.shape[0]), -np.inf)
+    for s in range(len(cu) - 1):
+        if lens[s] < 0:
+            continue
+        n = min(int(lens[s]) + cu[s + 1] - cu[s], room)
+        k, there = kv4_rows(k4, ks, pages[s], n)
+        v, _ = kv4_rows(v4, vs, pages[s], n)
+        for i in range(cu[s], cu[s + 1]):
+            see = there.copy()
+            see[int(lens[s]) + i - cu[s] + 1:] = False
+            if not see.any():
+                continue
+            for h in range(heads):
+                S = scale * (k[see, h // group] @ q[i, h])
+                if np.isnan(S).any() or np.isnan(v[see, h // group]).any():
+                    out[i, h], lse[h, i] = np.nan, np.nan
+                    continue
+                m = S.max()
+                e = np.exp(S - m)
+                out[i, h] = (e / e.sum()) @ v[see, h // group]
+                lse[h, i] = m + np.log(e.sum())
+    return out, lse

@@ -24,7 +24,8 @@ VFM_MAX_SEQS = 256
 
 EXPORTS = ("vfm_rope3d", "vfm_qknorm_rope3d", "vfm_qknorm_rope3d_bwd", "vfm_attn_fwd", "vfm_attn_bwd_workspace_size", "vfm_attn_bwd", "vfm_attn_bwd_noalloc", "vfm_xattn_fwd", "vfm_xattn_bwd_workspace_size", "vfm_xattn_bwd", "vfm_tattn_fwd", "vfm_tattn_bwd",
            "vfm_fp8_pack_sizes", "vfm_fp8_pack", "vfm_attn_fwd_fp8", "vfm_strerror", "vfm_last_hip_error", "vfm_schedule_units",
-           "vfm_attn_fwd_tile_rows")
+           "vfm_attn_fwd_tile_rows", "vfm_cattn_fwd_workspace_size", "vfm_cattn_fwd", "vfm_cattn_bwd_workspace_size", "vfm_cattn_bwd",
+           "vfm_kv4_append", "vfm_kv4_gather", "vfm_kv4_attn_workspace_size", "vfm_kv4_attn")
 
 _lib = None
 _calls = None                # the library's functions as the wrappers call them (load_library)
@@ -111,6 +112,29 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vfm_attn_fwd_tile_rows.argtypes = [p_i32, c_int, c_int, c_int, c_int, ctypes.POINTER(c_int)]
     lib.vfm_last_hip_error.restype = ctypes.c_char_p
     lib.vfm_last_hip_error.argtypes = []
+    c_i64 = ctypes.c_int64
+    causal_sizes = [p_i32, p_i32, c_int, c_int, c_int, c_int, c_int, c_int]
+    rows3 = [c_void_p, c_i64, c_void_p, c_i64, c_void_p, c_i64]          # three tensors with their token strides
+    lib.vfm_cattn_fwd_workspace_size.restype = c_size_t
+    lib.vfm_cattn_fwd_workspace_size.argtypes = causal_sizes
+    lib.vfm_cattn_fwd.restype = c_int
+    lib.vfm_cattn_fwd.argtypes = [*rows3, *causal_sizes, c_float, c_void_p, c_void_p, c_void_p, c_size_t, c_int, c_void_p]
+    lib.vfm_cattn_bwd_workspace_size.restype = c_size_t
+    lib.vfm_cattn_bwd_workspace_size.argtypes = causal_sizes
+    lib.vfm_cattn_bwd.restype = c_int
+    lib.vfm_cattn_bwd.argtypes = [*rows3, c_void_p, c_void_p, c_void_p, *causal_sizes, c_float, *rows3, c_void_p, c_size_t,
+                                  c_int, c_void_p]
+    cache = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int]       # k4, v4, k_scales, v_scales, n_pages, page_size
+    lib.vfm_kv4_append.restype = c_int
+    lib.vfm_kv4_append.argtypes = [c_void_p, c_i64, c_void_p, c_i64, p_i32, c_int, c_int, c_void_p, c_void_p, c_int, *cache,
+                                   c_int, c_int, c_int, c_void_p]
+    lib.vfm_kv4_gather.restype = c_int
+    lib.vfm_kv4_gather.argtypes = [*cache, c_void_p, c_int, p_i32, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_int, c_void_p]
+    lib.vfm_kv4_attn_workspace_size.restype = c_size_t
+    lib.vfm_kv4_attn_workspace_size.argtypes = [p_i32, c_int, c_int, c_int, c_int, c_int]
+    lib.vfm_kv4_attn.restype = c_int
+    lib.vfm_kv4_attn.argtypes = [c_void_p, c_i64, *cache, c_void_p, c_int, c_void_p, p_i32, c_int, c_int, c_int, c_int, c_int,
+                                 c_float, c_void_p, c_void_p, c_void_p, c_size_t, c_int, c_void_p]
     # The same functions taking a host int32 array as the address of its first element (a plain int, which the
     # wrappers below pass: see _host_i32); the library's own keep refusing anything but an int32 array or pointer.
     lib.by_address = types.SimpleNamespace()
@@ -418,4 +442,213 @@ def vfm_attn_fwd_fp8(q8, k8, vT8, scales, cu_seqlens, n_heads: int, head_dim: in
     _check(lib.vfm_attn_fwd_fp8(_dev(q8, "q8"), _dev(k8, "k8"), _dev(vT8, "vT8"), _dev(scales, "scales"), _i32_ptr(cu),
                                 int(cu.size - 1), total, int(n_heads), int(head_dim), _dev(out, "out"),
                                 _dev(lse, "lse"), _stream_ptr(stream)))
+    return out, lse
+
+
+# ---- causal attention with grouped heads, 4-bit key/value cache
+def _rows(t, name: str):
+    """Address and token stride of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart (a part of a wider one)."""
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name} must be a [tokens, heads, head_dim] device tensor")
+    if t.dtype is not _torch.bfloat16:
+        raise ValueError(f"{name} must be bfloat16, not {t.dtype}")
+    n, heads, hd = t.shape
+    if n == 0:
+        return t.data_ptr(), heads * hd
+    row, head, elem = t.stride()
+    if n == 1:                  # (a stride that no token takes)
+        row = heads * hd
+    if (elem != 1 and hd > 1) or (head != hd and heads > 1):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.data_ptr(), row
+
+
+def _like(t, name: str, shape, dtype) -> int:
+    """Address of a contiguous device tensor of exactly this shape and type."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    if t.dtype is not dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _on_current_device(*tensors) -> None:
+    """A kernel is launched on the current device: every tensor of the call has to live there."""
+    here = _torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"a tensor of the call lives on {t.device}, the current device is cuda:{here}")
+
+
+def _used_on(stream, *tensors) -> None:
+    """Tensors allocated here belong to the current stream; if the kernels run on another, tell the allocator."""
+    if stream is None:
+        return
+    s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream))
+    if s.cuda_stream == _torch.cuda.current_stream().cuda_stream:
+        return
+    for t in tensors:
+        if t.numel():
+            t.record_stream(s)
+
+
+def _workspace(given, need: int, like, stream):
+    """Address and size of the caller's workspace, or of one allocated for this call (kept alive by the third value)."""
+    if given is None:
+        if need == 0:
+            return 0, 0, None
+        given = _torch.empty(need, dtype=_torch.uint8, device=like.device)
+        _used_on(stream, given)
+    return _dev(given, "workspace"), given.numel() * given.element_size(), given
+
+
+def _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv):
+    cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
+    if cq.size != ck.size or cq.size < 1:
+        raise ValueError("cu_seqlens_q and cu_seqlens_kv must have the same length")
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("q [total_q, heads, head_dim], k and v [total_kv, kv_heads, head_dim] expected")
+    total_q, heads, hd = q.shape
+    return cq, ck, (_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, total_q, k.shape[0], heads, k.shape[1], hd)
+
+
+def vfm_cattn_fwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    lib = _calls or load_library().by_address
+    cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
+    return int(lib.vfm_cattn_fwd_workspace_size(_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, int(cq[-1]), int(ck[-1]), int(n_heads),
+                                                int(n_kv_heads), int(head_dim)))
+
+
+def vfm_cattn_fwd(q, k, v, cu_seqlens_q, cu_seqlens_kv, scale: float, out=None, lse=None, workspace=None, stream=None) -> Tuple:
+    """Causal attention with grouped heads: out[total_q, heads, head_dim] (bf16), lse[heads, total_q] (fp32).  k, v:
+    [total_kv, kv_heads, head_dim]; the last query of a sequence sees its last key.  q, k, v may be parts of one
+    tensor (tokens apart, a token's heads contiguous)."""
+    lib = _calls or load_library().by_address
+    cq, ck, sizes = _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv)
+    _on_current_device(q, k, v, out, lse, workspace)
+    total_q, heads, hd = q.shape
+    if out is None:
+        out = _torch.empty((total_q, heads, hd), dtype=_torch.bfloat16, device=q.device)
+        _used_on(stream, out)
+    if lse is None:
+        lse = _torch.empty((heads, total_q), dtype=_torch.float32, device=q.device)
+        _used_on(stream, lse)
+    ws, ws_bytes, keep = _workspace(workspace, 0 if workspace is not None else int(lib.vfm_cattn_fwd_workspace_size(*sizes)), q, stream)
+    _check(lib.vfm_cattn_fwd(*_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), *sizes, float(scale),
+                             _like(out, "out", (total_q, heads, hd), _torch.bfloat16),
+                             _like(lse, "lse", (heads, total_q), _torch.float32), ws, ws_bytes, VFM_BF16, _stream_ptr(stream)))
+    return out, lse
+
+
+def vfm_cattn_bwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    lib = _calls or load_library().by_address
+    cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
+    return int(lib.vfm_cattn_bwd_workspace_size(_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, int(cq[-1]), int(ck[-1]), int(n_heads),
+                                                int(n_kv_heads), int(head_dim)))
+
+
+def vfm_cattn_bwd(q, k, v, out, lse, dout, cu_seqlens_q, cu_seqlens_kv, scale: float, dq=None, dk=None, dv=None,
+                  workspace=None, stream=None) -> Tuple:
+    """Gradients of vfm_cattn_fwd: dq (shape of q), dk, dv (shape of k), bf16; given ones may be parts of one tensor."""
+    lib = _calls or load_library().by_address
+    cq, ck, sizes = _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv)
+    _on_current_device(q, k, v, out, lse, dout, dq, dk, dv, workspace)
+    total_q, heads, hd = q.shape
+    grads = []
+    for g, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
+        if g is None:
+            g = _torch.empty(like.shape, dtype=_torch.bfloat16, device=like.device)
+            _used_on(stream, g)
+        elif g.shape != like.shape:
+            raise ValueError(f"{name} must have shape {tuple(like.shape)}")
+        grads.append(g)
+    ws, ws_bytes, keep = _workspace(workspace, 0 if workspace is not None else int(lib.vfm_cattn_bwd_workspace_size(*sizes)), q, stream)
+    _check(lib.vfm_cattn_bwd(*_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), _like(out, "out", (total_q, heads, hd), _torch.bfloat16),
+                             _like(lse, "lse", (heads, total_q), _torch.float32),
+                             _like(dout, "dout", (total_q, heads, hd), _torch.bfloat16), *sizes, float(scale),
+                             *_rows(grads[0], "dq"), *_rows(grads[1], "dk"), *_rows(grads[2], "dv"), ws, ws_bytes, VFM_BF16,
+                             _stream_ptr(stream)))
+    return tuple(grads)
+
+
+def _kv4_cache(k4, v4, k_scales, v_scales):
+    """Addresses and sizes of a cache: (k4, v4, k_scales, v_scales, n_pages, page_size), kv_heads, head_dim."""
+    n_pages, kvh, page, half = k4.shape
+    hd = 2 * half
+    args = [_like(t, n, shape, _torch.uint8) for t, n, shape in (
+        (k4, "k4", (n_pages, kvh, page, half)), (v4, "v4", (n_pages, kvh, page, half)),
+        (k_scales, "k_scales", (n_pages, kvh, page, hd // 32)), (v_scales, "v_scales", (n_pages, kvh, page, hd // 32)))]
+    return (*args, n_pages, page), kvh, hd
+
+
+def _kv4_tables(pages, lens, n_seqs: int):
+    max_pages = pages.shape[1] if pages.dim() == 2 else -1
+    p = _like(pages, "pages", (n_seqs, max_pages), _torch.int32)
+    return p, max_pages, None if lens is None else _like(lens, "lens", (n_seqs,), _torch.int32)
+
+
+def vfm_kv4_append(k, v, k4, v4, k_scales, v_scales, pages, lens, cu_seqlens, stream=None) -> None:
+    """Quantises k, v [total, kv_heads, head_dim] (bf16, tokens may lie apart) into the paged 4-bit cache at the places
+    lens[s], lens[s] + 1, ... of their sequences.  pages [n_seqs, max_pages] and lens [n_seqs]: int32 on the device."""
+    lib = _calls or load_library().by_address
+    cu = _host_i32(cu_seqlens)
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
+    p, max_pages, n = _kv4_tables(pages, lens, cu.size - 1)
+    _on_current_device(k, v, k4, v4, k_scales, v_scales, pages, lens)
+    if k.shape != v.shape or tuple(k.shape[1:]) != (kvh, hd):
+        raise ValueError(f"k and v must be [total, {kvh}, {hd}]")
+    _check(lib.vfm_kv4_append(*_rows(k, "k"), *_rows(v, "v"), _i32_ptr(cu), cu.size - 1, k.shape[0], n, p, max_pages, *cache, kvh, hd,
+                              VFM_BF16, _stream_ptr(stream)))
+
+
+def vfm_kv4_gather(k4, v4, k_scales, v_scales, pages, cu_seqlens, k=None, v=None, stream=None) -> Tuple:
+    """The first cu_seqlens[s+1] - cu_seqlens[s] places of every sequence as bf16 k, v [total, kv_heads, head_dim]."""
+    lib = _calls or load_library().by_address
+    cu = _host_i32(cu_seqlens)
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
+    p, max_pages, _ = _kv4_tables(pages, None, cu.size - 1)
+    _on_current_device(k4, v4, k_scales, v_scales, pages, k, v)
+    total = int(cu[-1])
+    if k is None:
+        k = _torch.empty((total, kvh, hd), dtype=_torch.bfloat16, device=k4.device)
+        _used_on(stream, k)
+    if v is None:
+        v = _torch.empty((total, kvh, hd), dtype=_torch.bfloat16, device=k4.device)
+        _used_on(stream, v)
+    _check(lib.vfm_kv4_gather(*cache, p, max_pages, _i32_ptr(cu), cu.size - 1, total, kvh, hd,
+                              _like(k, "k", (total, kvh, hd), _torch.bfloat16), _like(v, "v", (total, kvh, hd), _torch.bfloat16),
+                              VFM_BF16, _stream_ptr(stream)))
+    return k, v
+
+
+def vfm_kv4_attn_workspace_size(cu_seqlens, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    lib = _calls or load_library().by_address
+    cu = _host_i32(cu_seqlens)
+    return int(lib.vfm_kv4_attn_workspace_size(_i32_ptr(cu), cu.size - 1, int(cu[-1]), int(n_heads), int(n_kv_heads), int(head_dim)))
+
+
+def vfm_kv4_attn(q, k4, v4, k_scales, v_scales, pages, lens, cu_seqlens, scale: float, out=None, lse=None, workspace=None,
+                 stream=None) -> Tuple:
+    """Attention of the new tokens q [total, heads, head_dim] (bf16, tokens may lie apart) over the 4-bit cache, which holds
+    their own keys and values already: token t of sequence s sees the places 0 .. lens[s] + t.  Returns out (bf16) and
+    lse [heads, total] (fp32)."""
+    lib = _calls or load_library().by_address
+    cu = _host_i32(cu_seqlens)
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
+    p, max_pages, n = _kv4_tables(pages, lens, cu.size - 1)
+    _on_current_device(q, k4, v4, k_scales, v_scales, pages, lens, out, lse, workspace)
+    if q.dim() != 3 or q.shape[2] != hd:
+        raise ValueError(f"q must be [total, heads, {hd}]")
+    total, heads, _ = q.shape
+    if out is None:
+        out = _torch.empty((total, heads, hd), dtype=_torch.bfloat16, device=q.device)
+        _used_on(stream, out)
+    if lse is None:
+        lse = _torch.empty((heads, total), dtype=_torch.float32, device=q.device)
+        _used_on(stream, lse)
+    need = 0 if workspace is not None else int(lib.vfm_kv4_attn_workspace_size(_i32_ptr(cu), cu.size - 1, total, heads, kvh, hd))
+    ws, ws_bytes, keep = _workspace(workspace, need, q, stream)
+    _check(lib.vfm_kv4_attn(*_rows(q, "q"), *cache, p, max_pages, n, _i32_ptr(cu), cu.size - 1, total, heads, kvh, hd, float(scale),
+                            _like(out, "out", (total, heads, hd), _torch.bfloat16), _like(lse, "lse", (heads, total), _torch.float32),
+                            ws, ws_bytes, VFM_BF16, _stream_ptr(stream)))
     return out, lse

@@ -1,0 +1,377 @@
+// Causal packed attention forward with grouped heads for gfx950 (bf16 MFMA, fp32 accumulate).
+//
+//     S_ij = scale q_i . k_j  (j <= i + off),   out_i = sum_j softmax_j(S_ij) v_j,   lse_i = ln sum_j exp(S_ij)
+//
+// One workgroup owns a tile of rows (query token x head of the group, see cattn_common.h) of one (sequence, K/V head), 32 rows
+// per wavefront, and streams the keys that its last row sees through LDS in units of 32.  The loop is that of the
+// bidirectional forward (attn_fwd.hip): S^T = K Q^T so that a lane holds 16 keys of one row, P^T is the B operand of
+// O^T += V^T P^T as it stands, S(u+1) and O += V(u-1) P(u-1) run under the softmax of unit u, the softmax reference moves only when
+// a unit's exponentials would grow too large, K and V in rings of four LDS slots.  What the causal order adds: a wavefront masks only the
+// units that reach past its first row's limit, computes none past its last row's (it keeps fetching its share and
+// meeting the barriers for the wavefronts behind it), and row tiles are handed out longest first.
+#include "cattn_common.h"
+
+namespace vfm {
+
+constexpr int kCU = 32;                 // keys per pipeline unit
+constexpr int kCRing = 4;               // LDS ring slots for K and for V
+constexpr float kCLog2e = 1.4426950408889634f;
+constexpr float kCLn2 = 0.6931471805599453f;
+constexpr float kCSafeSum = 256.0f;     // a unit's exponentials may sum to this before the reference moves
+
+template <int D, int W>
+struct CFwdCfg {
+  static constexpr int kRows = W * 32;
+  static constexpr int kUnitBytes = kCU * D * 2;
+  static constexpr int kQBase = (2 * kCRing - 2) * kUnitBytes;     // Q rows: over the V ring's last two slots and behind
+  static constexpr int kLdsBytes = kQBase + kRows * D * 2;
+  static_assert(kRows * D * 2 >= 2 * kUnitBytes && kLdsBytes <= 160 * 1024, "rings, LDS of one CU");
+  static constexpr int kChunksPerRow = D / 8;
+  static constexpr int kLoadsPerWave = kCU * kChunksPerRow / (W * 64);
+};
+
+constexpr int kSgcValu = 0x002, kSgcMfma = 0x008, kSgcDsRead = 0x100;
+
+template <int D, int W>
+__global__ __launch_bounds__(W * 64, D == 64 ? 3 : 2)
+void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                      __bf16* __restrict__ out, float* __restrict__ lse, const XSegTable segs, const TileIndex ti,
+                      const CausalShape sh) {
+  using Cfg = CFwdCfg<D, W>;
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int LPW = Cfg::kLoadsPerWave;
+  constexpr int UB = Cfg::kUnitBytes;
+  constexpr int RB = D * 2;
+  constexpr int kInFlight = 2 * 2 * LPW;
+
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+
+  // workgroup b: all K/V heads of one tile before the next (heads on consecutive XCDs: an XCD keeps to its heads), a
+  // sequence's last tile, which sees most, first
+  const int kvh = blockIdx.x % sh.n_kv_heads;
+  int seq, tq;
+  locate_tile(ti, segs.n, blockIdx.x / sh.n_kv_heads, seq, tq);
+  const CausalSeq cs = causal_seq(segs, seq, sh.group);
+  tq = (cs.rows + Cfg::kRows - 1) / Cfg::kRows - 1 - tq;
+  const int r0 = tq * Cfg::kRows;                               // first row of the tile
+
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const int c = lane & 31;
+  const int g = lane >> 5;
+
+  const int row_w = r0 + wave * 32;                             // the wavefront's first row
+  const int rows_valid = cs.rows - row_w;                       // may be <= 0, or more than 32
+  auto row_tok = [&](int r) { return r / sh.group; };
+  const int my_row = min(row_w + c, cs.rows - 1);
+  const int my_tok = row_tok(my_row);
+  const int my_head = kvh * sh.group + (my_row - my_tok * sh.group);
+  const int lim = my_tok + cs.off;                              // this lane's row sees keys <= lim
+  // keys that the tile, and this wavefront, look at
+  const int n_keys = row_tok(min(r0 + Cfg::kRows, cs.rows) - 1) + cs.off + 1;
+  const int n_units = n_keys > 0 ? (n_keys + kCU - 1) / kCU : 0;
+  const int wave_min = __builtin_amdgcn_readfirstlane(row_tok(min(row_w, cs.rows - 1)) + cs.off);   // its first row's limit
+  const int wave_last = row_tok(min(row_w + 32, cs.rows) - 1) + cs.off;
+  const int wave_units = __builtin_amdgcn_readfirstlane(rows_valid <= 0 || wave_last < 0 ? 0 : wave_last / kCU + 1);
+
+  // address of row r of the wavefront's tile in out
+  auto out_row = [&](int r) {
+    const int row = row_w + r, tok = row_tok(row);
+    return out + ((size_t)(cs.qs + tok) * sh.n_heads + kvh * sh.group + (row - tok * sh.group)) * D;
+  };
+  auto write_empty = [&]() {                                    // rows that see no key
+    if (row_w + c < cs.rows && g == 0) lse[(size_t)my_head * sh.total_q + cs.qs + my_tok] = -INFINITY;
+    const u32x4 z = {0u, 0u, 0u, 0u};
+    for (int i = lane; i < 32 * Cfg::kChunksPerRow; i += 64) {
+      const int r = i / Cfg::kChunksPerRow;
+      if (r < rows_valid) *reinterpret_cast<u32x4*>(out_row(r) + (i % Cfg::kChunksPerRow) * 8) = z;
+    }
+  };
+  if (n_units == 0) { write_empty(); return; }
+
+  // ---- K/V staging with direct global->LDS loads (as in attn_fwd.hip); byte offsets count from the sequence's first
+  // key; keys past the last one clamp to it (no row sees them)
+  const char* kbase = uniform_ptr(reinterpret_cast<const char*>(k) + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB);
+  const char* vbase = uniform_ptr(reinterpret_cast<const char*>(v) + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB);
+  const uint32_t k_last = (uint32_t)(cs.kl - 1) * sh.k_row, v_last = (uint32_t)(cs.kl - 1) * sh.v_row;
+  uint32_t st_colb[LPW], k_rowoff[LPW], v_rowoff[LPW];
+#pragma unroll
+  for (int x = 0; x < LPW; ++x) {
+    const int p = (x * W + wave) * 64 + lane;
+    const int r = p / Cfg::kChunksPerRow;
+    k_rowoff[x] = (uint32_t)r * sh.k_row;
+    v_rowoff[x] = (uint32_t)r * sh.v_row;
+    st_colb[x] = (uint32_t)(((p % Cfg::kChunksPerRow) ^ swz<D>(r)) * 16);
+  }
+  const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + wave * 1024);
+  auto issue_k = [&](int slot) {
+#pragma unroll
+    for (int x = 0; x < LPW; ++x) {
+      lds_dma16(kbase, min(k_rowoff[x], k_last) + st_colb[x], wave_lds + slot * UB + x * W * 1024);
+      k_rowoff[x] += kCU * sh.k_row;
+    }
+  };
+  auto issue_v = [&](int slot) {
+#pragma unroll
+    for (int x = 0; x < LPW; ++x) {
+      lds_dma16(vbase, min(v_rowoff[x], v_last) + st_colb[x], wave_lds + (kCRing + slot) * UB + x * W * 1024);
+      v_rowoff[x] += kCU * sh.v_row;
+    }
+  };
+  // units that this wavefront does not compute: its share of the requests, the wait, the barrier
+  auto idle_unit = [&](int u) {
+    issue_k((u + 1) % kCRing);
+    issue_v((u + 2) % kCRing);
+    wait_vmcnt<kInFlight>();
+    __syncthreads();
+  };
+
+  if (wave_units == 0) {
+    issue_k(0); issue_k(1); issue_k(2); issue_k(3);
+    issue_v(0); issue_v(1);
+    wait_vmcnt<0>();
+    __syncthreads();
+    __syncthreads();
+    issue_k(0);
+    for (int u = 0; u < n_units; ++u) idle_unit(u);
+    wait_vmcnt<0>();
+    __syncthreads();
+    write_empty();
+    return;
+  }
+
+  const int kbase_off = tile_off<D>(c, 8 * g);
+  int vbase_off[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    vbase_off[t] = tile_off<D>(8 * t + 4 * g + ((lane & 15) >> 2), 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+
+  const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  f32x16 oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = zero16;
+
+  auto read_k = [&](int slot, bf16x8 (&ka)[KS]) {
+    const char* kt = smem + slot * UB;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = lds_read_b128(kt, kbase_off ^ (ks << 5));
+  };
+  auto mask = [&](int u, f32x16& s) {    // keys that the lane's row does not see
+    const int j0 = u * kCU;
+    if (j0 + kCU - 1 > wave_min) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (j0 + 8 * (r >> 2) + 4 * g + (r & 3) > lim) s[r] = -INFINITY;
+    }
+  };
+
+  // ---- prologue: Q rows, K units 0..3 and V units 0..1; S(0); operands of K(1)
+  const uint32_t q_lds = lds_addr_of(smem) + Cfg::kQBase + wave * (32 * RB);
+  {
+    const char* qbase = uniform_ptr(reinterpret_cast<const char*>(q) + (size_t)cs.qs * sh.q_row + (size_t)kvh * sh.group * RB);
+    const uint32_t q_s = __builtin_amdgcn_readfirstlane(q_lds);
+#pragma unroll
+    for (int x = 0; x < 32 * RB / 1024; ++x) {
+      const int p = x * 64 + lane, r = p / Cfg::kChunksPerRow;
+      const int row = min(row_w + r, cs.rows - 1), tok = row_tok(row);
+      lds_dma16(qbase, (uint32_t)tok * sh.q_row + (uint32_t)(row - tok * sh.group) * RB +
+                           (uint32_t)(((p % Cfg::kChunksPerRow) ^ swz<D>(r)) * 16), q_s + x * 1024);
+    }
+  }
+  issue_k(0); issue_k(1); issue_k(2); issue_k(3);
+  issue_v(0); issue_v(1);
+  wait_vmcnt<0>();
+  bf16x8 qreg[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    qreg[ks] = lds_read_b128_at(q_lds + (kbase_off ^ (ks << 5)));
+    settle(qreg[ks]);
+  }
+  __syncthreads();
+
+  bf16x8 ka[KS];
+  f32x16 s_cur;
+  {
+    bf16x8 k0[KS];
+    read_k(0, k0);
+    read_k(1, ka);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) s_cur = mfma32(k0[ks], qreg[ks], ks == 0 ? zero16 : s_cur);
+    mask(0, s_cur);
+  }
+  // first reference point: the row maximum of unit 0 (a row that sees any key sees key 0); 0 for a row that sees none
+  float m_run, l_run = 0.f;
+  {
+    float mx = s_cur[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s_cur[r]);
+    m_run = pair_max(mx) * sh.scale_log2;
+    if (m_run == -INFINITY) m_run = 0.f;
+  }
+  __syncthreads();            // every wave holds K(0), K(1) in registers: slots 0, 1 are free
+  issue_k(0);                 // K unit 4
+
+  bf16x8 pb_prev[2];
+  pb_prev[0] = pb_prev[1] = bf16x8{};
+
+  auto iteration = [&](auto slot_c, auto pv_c, int u) {
+    constexpr int SLOT = decltype(slot_c)::value;
+    constexpr bool PV = decltype(pv_c)::value != 0;
+    issue_k((SLOT + 1) % kCRing);     // K(u+5)
+    issue_v((SLOT + 2) % kCRing);     // V(u+2)
+
+    // ---- region 1: S(u+1) MFMAs | V(u-1) operand reads | first half of softmax(u)
+    s16x4 vlo[2][DB], vhi[2][DB];
+    if constexpr (PV) {
+      const char* vt = smem + (kCRing + (SLOT + 3) % kCRing) * UB;
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          vlo[s2][db] = lds_read_tr(vt, (vbase_off[0] ^ (db << 6)) + 16 * s2 * RB);
+          vhi[s2][db] = lds_read_tr(vt, (vbase_off[1] ^ (db << 6)) + 16 * s2 * RB);
+        }
+    }
+    f32x16 s_next, s_odd;     // two accumulation chains: a single one cannot issue back to back
+#pragma unroll
+    for (int ks = 0; ks < KS; ks += 2) {
+      s_next = mfma32(ka[ks], qreg[ks], ks == 0 ? zero16 : s_next);
+      s_odd = mfma32(ka[ks + 1], qreg[ks + 1], ks == 0 ? zero16 : s_odd);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s_next[r] += s_odd[r];
+
+    f32x8 p0, p1;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p0[r] = fast_exp2(s_cur[r] * sh.scale_log2 - m_run);
+    bf16x8 pb_cur[2];
+    pb_cur[0] = to_bf16x8(p0);
+    float lsum = 0.f;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) lsum += p0[r];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSgcMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgcDsRead, PV ? 2 : 0, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgcValu, 5, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- region 2: O += V(u-1) P(u-1) MFMAs | K(u+2) operand reads | second half of softmax(u)
+    if constexpr (PV) {
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          oacc[db] = mfma32(join_tr(vlo[s2][db], vhi[s2][db]), pb_prev[s2], oacc[db]);
+    }
+    bf16x8 ka_next[KS];
+    read_k((SLOT + 2) % kCRing, ka_next);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) p1[r] = fast_exp2(s_cur[8 + r] * sh.scale_log2 - m_run);
+    pb_cur[1] = to_bf16x8(p1);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) lsum += p1[r];
+    const bool redo = __builtin_amdgcn_ballot_w64(!(lsum <= kCSafeSum)) != 0;
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSgcMfma, PV ? 1 : 0, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgcDsRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgcValu, 4, 0);
+    }
+    asm volatile("" : "+v"(pb_cur[0]), "+v"(pb_cur[1]), "+v"(lsum));
+    __builtin_amdgcn_sched_barrier(0);
+
+    // rare (wave-uniform): move the reference to the true running maximum and bring everything to it
+    if (redo) {
+      float mx = s_cur[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s_cur[r]);
+      const float m_new = fmaxf(m_run, pair_max(mx) * sh.scale_log2);
+      const float alpha = fast_exp2(m_run - m_new);
+      m_run = m_new;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        p0[r] = fast_exp2(s_cur[r] * sh.scale_log2 - m_new);
+        p1[r] = fast_exp2(s_cur[8 + r] * sh.scale_log2 - m_new);
+      }
+      pb_cur[0] = to_bf16x8(p0);
+      pb_cur[1] = to_bf16x8(p1);
+      lsum = 0.f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) lsum += p0[r] + p1[r];
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+    }
+    l_run += lsum;
+
+    mask(u + 1, s_next);
+    s_cur = s_next;
+    pb_prev[0] = pb_cur[0];
+    pb_prev[1] = pb_cur[1];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) ka[ks] = ka_next[ks];
+
+    wait_vmcnt<kInFlight>();   // everything but the two youngest batches has landed ...
+    __syncthreads();           // ... for every wave, and every wave is done with this unit's slots
+  };
+
+  iteration(IntC<0>{}, IntC<0>{}, 0);
+  for (int u = 1; u < wave_units; u += 4) {
+    iteration(IntC<1>{}, IntC<1>{}, u);
+    if (u + 1 < wave_units) iteration(IntC<2>{}, IntC<1>{}, u + 1);
+    if (u + 2 < wave_units) iteration(IntC<3>{}, IntC<1>{}, u + 2);
+    if (u + 3 < wave_units) iteration(IntC<0>{}, IntC<1>{}, u + 3);
+  }
+  // ---- drain: accumulate the wavefront's last unit (its slot is taken again two units on, a barrier away)
+  {
+    const char* vt = smem + (kCRing + (wave_units - 1) % kCRing) * UB;
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 va = join_tr(lds_read_tr(vt, (vbase_off[0] ^ (db << 6)) + 16 * s2 * RB),
+                                  lds_read_tr(vt, (vbase_off[1] ^ (db << 6)) + 16 * s2 * RB));
+        oacc[db] = mfma32(va, pb_prev[s2], oacc[db]);
+      }
+  }
+  for (int u = wave_units; u < n_units; ++u) idle_unit(u);
+  wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
+
+  // ---- epilogue: normalise, write out (bf16) and lse (natural log); a row without keys: 0 and -inf
+  const float l_tot = pair_sum(l_run);
+  const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
+  if (row_w + c < cs.rows && g == 0)
+    lse[(size_t)my_head * sh.total_q + cs.qs + my_tok] = lim < 0 ? -INFINITY : (m_run + __log2f(l_tot)) * kCLn2;
+  __syncthreads();   // the rings are free: each wavefront turns its tile through a piece of them
+  store_tile_rows_at<D>(smem + wave * (32 * RB), oacc, inv, rows_valid, out_row);
+}
+
+template <int D, int W>
+static hipError_t launch_cfg(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
+                             void* out, float* lse, hipStream_t stream) {
+  using Cfg = CFwdCfg<D, W>;
+  const TileIndex ti = make_causal_index<false>(segs, sh.group, Cfg::kRows);
+  const int tiles = count_tiles(ti);
+  if (tiles == 0) return hipSuccess;
+  auto kern = cattn_fwd_kernel<D, W>;
+  hipError_t e = allow_lds(kern, Cfg::kLdsBytes);
+  if (e != hipSuccess) return e;
+  return launch(kern, dim3((unsigned)tiles * sh.n_kv_heads), dim3(W * 64), Cfg::kLdsBytes, stream, (const __bf16*)q,
+                (const __bf16*)k, (const __bf16*)v, (__bf16*)out, lse, segs, ti, sh);
+}
+
+hipError_t launch_cattn_fwd(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
+                            int head_dim, void* out, float* lse, hipStream_t stream) {
+  if (head_dim == 64) return launch_cfg<64, 4>(q, k, v, segs, sh, out, lse, stream);
+  int longest = 0;
+  for (int s = 0; s < segs.n; ++s) longest = longest > segs.kl[s] ? longest : segs.kl[s];
+  if (longest <= 1024) return launch_cfg<128, 4>(q, k, v, segs, sh, out, lse, stream);
+  return launch_cfg<128, 8>(q, k, v, segs, sh, out, lse, stream);
+}
+
+}  // namespace vfm

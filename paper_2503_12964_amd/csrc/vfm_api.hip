@@ -239,6 +239,8 @@ hipError_t scratch_of_current_device(void** out) {
 
 }  // namespace
 
+int vfm::launch_status(hipError_t e) { return ::launch_status(e); }
+
 extern "C" {
 
 const char* vfm_last_hip_error(void) { return hipGetErrorString(g_last_hip_error); }
@@ -256,6 +258,8 @@ const char* vfm_strerror(int status) {
     case VFM_ERR_LAUNCH: return "the HIP runtime refused a kernel launch";
     case VFM_ERR_ALIGN: return "tensor pointers must be 16-byte aligned";
     case VFM_ERR_SCRATCH: return "n_heads * total_tokens exceeds VFM_NOALLOC_MAX_ROWS, the capacity of the built-in scratch of vfm_attn_bwd_noalloc (use vfm_attn_bwd with a workspace)";
+    case VFM_ERR_STRIDE: return "a token stride must be a multiple of 8 elements and at least heads * head_dim";
+    case VFM_ERR_PAGE: return "page_size must be a power of two from 16 to 2^20, n_pages and max_pages >= 0";
     default: return "unknown status";
   }
 }

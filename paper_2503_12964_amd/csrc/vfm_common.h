@@ -679,6 +679,9 @@ inline hipError_t allow_lds(void (*kern)(P...), int bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
 
+// vfm_status of a launch; keeps the error for vfm_last_hip_error.
+int launch_status(hipError_t e);
+
 // ---- launchers (defined next to their kernels) -----------------------------
 // Compute units of the current device (asked once; 256 on MI355X, also the fallback).
 int compute_unit_count();
