@@ -446,70 +446,94 @@ def vfm_attn_fwd_fp8(q8, k8, vT8, scales, cu_seqlens, n_heads: int, head_dim: in
 
 
 # ---- causal attention with grouped heads, 4-bit key/value cache
-def _rows(t, name: str):
-    """Address and token stride of a [tokens, heads, head_dim] bf16 tensor whose tokens may lie apart (a part of a wider one)."""
-    if t.dim() != 3 or not t.is_cuda:
-        raise ValueError(f"{name} must be a [tokens, heads, head_dim] device tensor")
-    if t.dtype is not _torch.bfloat16:
-        raise ValueError(f"{name} must be bfloat16, not {t.dtype}")
-    n, heads, hd = t.shape
-    if n == 0:
+# What a call costs here bounds the smallest steps (a token of one sequence: 11 us on the GPU), so each argument is looked at once:
+# its device (which also tells a host tensor), type, shape and order, and what a wrapper allocates itself is not looked at.
+def _current_device() -> int:
+    try:
+        return _torch._C._cuda_getDevice()
+    except AttributeError:      # another PyTorch
+        return _torch.cuda.current_device()
+
+
+def _elsewhere(t, name: str, here: int):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    raise ValueError(f"{name} lives on {t.device}, the current device is cuda:{here}")
+
+
+def _rows(t, name: str, here: int, shape):
+    """Address and token stride of a bf16 tensor of this shape, [tokens, heads, head_dim], whose tokens may lie apart."""
+    if t.get_device() != here:
+        _elsewhere(t, name, here)
+    if t.dtype is not _torch.bfloat16 or t.shape != shape:
+        raise ValueError(f"{name} must be bfloat16 of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+    n, heads, hd = shape
+    if t.is_contiguous():
         return t.data_ptr(), heads * hd
     row, head, elem = t.stride()
-    if n == 1:                  # (a stride that no token takes)
-        row = heads * hd
     if (elem != 1 and hd > 1) or (head != hd and heads > 1):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.data_ptr(), row
+    return t.data_ptr(), row if n > 1 else heads * hd
 
 
-def _like(t, name: str, shape, dtype) -> int:
-    """Address of a contiguous device tensor of exactly this shape and type."""
-    if not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous device tensor")
-    if t.dtype is not dtype or tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
+def _like(t, name: str, here: int, shape, dtype) -> int:
+    """Address of a contiguous tensor of exactly this shape and type."""
+    if t.get_device() != here:
+        _elsewhere(t, name, here)
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
     return t.data_ptr()
 
 
-def _on_current_device(*tensors) -> None:
-    """A kernel is launched on the current device: every tensor of the call has to live there."""
-    here = _torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != here:
-            raise ValueError(f"a tensor of the call lives on {t.device}, the current device is cuda:{here}")
-
-
-def _used_on(stream, *tensors) -> None:
-    """Tensors allocated here belong to the current stream; if the kernels run on another, tell the allocator."""
-    if stream is None:
-        return
-    s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream))
-    if s.cuda_stream == _torch.cuda.current_stream().cuda_stream:
-        return
-    for t in tensors:
-        if t.numel():
+def _new(shape, dtype, like, stream):
+    """A tensor for the kernels of this call.  It belongs to the current stream; if they run on another, tell the allocator."""
+    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+        t = _torch.empty_like(like)          # (a third less than the general call)
+    else:
+        t = _torch.empty(shape, dtype=dtype, device=like.device)
+    if stream is not None and t.numel():
+        s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream))
+        if s.cuda_stream != _torch.cuda.current_stream().cuda_stream:
             t.record_stream(s)
+    return t
 
 
-def _workspace(given, need: int, like, stream):
-    """Address and size of the caller's workspace, or of one allocated for this call (kept alive by the third value)."""
+def _out_lse(q, shape, out, lse, here: int, stream):
+    """out and lse of a forward, and their addresses."""
+    total, heads, _ = shape
+    if out is None:
+        out = _new(shape, _torch.bfloat16, q, stream)
+        po = out.data_ptr()
+    else:
+        po = _like(out, "out", here, shape, _torch.bfloat16)
+    if lse is None:
+        lse = _new((heads, total), _torch.float32, q, stream)
+        return out, lse, po, lse.data_ptr()
+    return out, lse, po, _like(lse, "lse", here, (heads, total), _torch.float32)
+
+
+def _workspace(given, size, sizes, like, here: int, stream):
+    """The workspace (kept by the caller of this), its address and size: the one given, or one of size(*sizes) bytes."""
     if given is None:
-        if need == 0:
-            return 0, 0, None
-        given = _torch.empty(need, dtype=_torch.uint8, device=like.device)
-        _used_on(stream, given)
-    return _dev(given, "workspace"), given.numel() * given.element_size(), given
+        need = size(*sizes)
+        if not need:
+            return None, 0, 0
+        given = _new(need, _torch.uint8, like, stream)
+        return given, given.data_ptr(), need
+    if given.get_device() != here or not given.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor of the current device")
+    return given, given.data_ptr(), given.numel() * given.element_size()
 
 
-def _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv):
+def _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv):
     cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
     if cq.size != ck.size or cq.size < 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_kv must have the same length")
-    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or k.shape[2] != q.shape[2]:
+    sq, sk = q.shape, k.shape
+    if len(sq) != 3 or len(sk) != 3 or sk[2] != sq[2]:
         raise ValueError("q [total_q, heads, head_dim], k and v [total_kv, kv_heads, head_dim] expected")
-    total_q, heads, hd = q.shape
-    return cq, ck, (_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, total_q, k.shape[0], heads, k.shape[1], hd)
+    pq = _i32_ptr(cq)
+    return cq, ck, sq, sk, (pq, pq if ck is cq else _i32_ptr(ck), cq.size - 1, sq[0], sk[0], sq[1], sk[1], sq[2])
 
 
 def vfm_cattn_fwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
@@ -524,19 +548,12 @@ def vfm_cattn_fwd(q, k, v, cu_seqlens_q, cu_seqlens_kv, scale: float, out=None, 
     [total_kv, kv_heads, head_dim]; the last query of a sequence sees its last key.  q, k, v may be parts of one
     tensor (tokens apart, a token's heads contiguous)."""
     lib = _calls or load_library().by_address
-    cq, ck, sizes = _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv)
-    _on_current_device(q, k, v, out, lse, workspace)
-    total_q, heads, hd = q.shape
-    if out is None:
-        out = _torch.empty((total_q, heads, hd), dtype=_torch.bfloat16, device=q.device)
-        _used_on(stream, out)
-    if lse is None:
-        lse = _torch.empty((heads, total_q), dtype=_torch.float32, device=q.device)
-        _used_on(stream, lse)
-    ws, ws_bytes, keep = _workspace(workspace, 0 if workspace is not None else int(lib.vfm_cattn_fwd_workspace_size(*sizes)), q, stream)
-    _check(lib.vfm_cattn_fwd(*_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), *sizes, float(scale),
-                             _like(out, "out", (total_q, heads, hd), _torch.bfloat16),
-                             _like(lse, "lse", (heads, total_q), _torch.float32), ws, ws_bytes, VFM_BF16, _stream_ptr(stream)))
+    cq, ck, sq, sk, sizes = _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv)
+    here = _current_device()
+    rows = (*_rows(q, "q", here, sq), *_rows(k, "k", here, sk), *_rows(v, "v", here, sk))
+    out, lse, po, pl = _out_lse(q, sq, out, lse, here, stream)
+    workspace, pw, nw = _workspace(workspace, lib.vfm_cattn_fwd_workspace_size, sizes, q, here, stream)
+    _check(lib.vfm_cattn_fwd(*rows, *sizes, scale, po, pl, pw, nw, VFM_BF16, _stream_ptr(stream)))
     return out, lse
 
 
@@ -551,40 +568,38 @@ def vfm_cattn_bwd(q, k, v, out, lse, dout, cu_seqlens_q, cu_seqlens_kv, scale: f
                   workspace=None, stream=None) -> Tuple:
     """Gradients of vfm_cattn_fwd: dq (shape of q), dk, dv (shape of k), bf16; given ones may be parts of one tensor."""
     lib = _calls or load_library().by_address
-    cq, ck, sizes = _causal_sizes(q, k, v, cu_seqlens_q, cu_seqlens_kv)
-    _on_current_device(q, k, v, out, lse, dout, dq, dk, dv, workspace)
-    total_q, heads, hd = q.shape
-    grads = []
-    for g, like, name in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv")):
-        if g is None:
-            g = _torch.empty(like.shape, dtype=_torch.bfloat16, device=like.device)
-            _used_on(stream, g)
-        elif g.shape != like.shape:
-            raise ValueError(f"{name} must have shape {tuple(like.shape)}")
-        grads.append(g)
-    ws, ws_bytes, keep = _workspace(workspace, 0 if workspace is not None else int(lib.vfm_cattn_bwd_workspace_size(*sizes)), q, stream)
-    _check(lib.vfm_cattn_bwd(*_rows(q, "q"), *_rows(k, "k"), *_rows(v, "v"), _like(out, "out", (total_q, heads, hd), _torch.bfloat16),
-                             _like(lse, "lse", (heads, total_q), _torch.float32),
-                             _like(dout, "dout", (total_q, heads, hd), _torch.bfloat16), *sizes, float(scale),
-                             *_rows(grads[0], "dq"), *_rows(grads[1], "dk"), *_rows(grads[2], "dv"), ws, ws_bytes, VFM_BF16,
-                             _stream_ptr(stream)))
-    return tuple(grads)
+    cq, ck, sq, sk, sizes = _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv)
+    here, bf16 = _current_device(), _torch.bfloat16
+    rows = (*_rows(q, "q", here, sq), *_rows(k, "k", here, sk), *_rows(v, "v", here, sk))
+    given = (_like(out, "out", here, sq, bf16), _like(lse, "lse", here, (sq[1], sq[0]), _torch.float32), _like(dout, "dout", here, sq, bf16))
+    if dq is None:
+        dq = _new(sq, bf16, q, stream)
+    if dk is None:
+        dk = _new(sk, bf16, k, stream)
+    if dv is None:
+        dv = _new(sk, bf16, v, stream)
+    grads = (*_rows(dq, "dq", here, sq), *_rows(dk, "dk", here, sk), *_rows(dv, "dv", here, sk))
+    workspace, pw, nw = _workspace(workspace, lib.vfm_cattn_bwd_workspace_size, sizes, q, here, stream)
+    _check(lib.vfm_cattn_bwd(*rows, *given, *sizes, scale, *grads, pw, nw, VFM_BF16, _stream_ptr(stream)))
+    return dq, dk, dv
 
 
-def _kv4_cache(k4, v4, k_scales, v_scales):
+def _kv4_cache(k4, v4, k_scales, v_scales, here: int):
     """Addresses and sizes of a cache: (k4, v4, k_scales, v_scales, n_pages, page_size), kv_heads, head_dim."""
-    n_pages, kvh, page, half = k4.shape
-    hd = 2 * half
-    args = [_like(t, n, shape, _torch.uint8) for t, n, shape in (
-        (k4, "k4", (n_pages, kvh, page, half)), (v4, "v4", (n_pages, kvh, page, half)),
-        (k_scales, "k_scales", (n_pages, kvh, page, hd // 32)), (v_scales, "v_scales", (n_pages, kvh, page, hd // 32)))]
-    return (*args, n_pages, page), kvh, hd
+    shape, u8 = k4.shape, _torch.uint8
+    if len(shape) != 4:
+        raise ValueError("k4 must be [n_pages, kv_heads, page_size, head_dim / 2]")
+    n_pages, kvh, page, half = shape
+    blocks = (n_pages, kvh, page, half // 16)
+    return (_like(k4, "k4", here, shape, u8), _like(v4, "v4", here, shape, u8), _like(k_scales, "k_scales", here, blocks, u8),
+            _like(v_scales, "v_scales", here, blocks, u8), n_pages, page), kvh, 2 * half
 
 
-def _kv4_tables(pages, lens, n_seqs: int):
-    max_pages = pages.shape[1] if pages.dim() == 2 else -1
-    p = _like(pages, "pages", (n_seqs, max_pages), _torch.int32)
-    return p, max_pages, None if lens is None else _like(lens, "lens", (n_seqs,), _torch.int32)
+def _kv4_pages(pages, here: int, n_seqs: int):
+    shape = pages.shape
+    if len(shape) != 2:
+        raise ValueError("pages must be [n_seqs, max_pages]")
+    return _like(pages, "pages", here, (n_seqs, shape[1]), _torch.int32), shape[1]
 
 
 def vfm_kv4_append(k, v, k4, v4, k_scales, v_scales, pages, lens, cu_seqlens, stream=None) -> None:
@@ -592,32 +607,30 @@ def vfm_kv4_append(k, v, k4, v4, k_scales, v_scales, pages, lens, cu_seqlens, st
     lens[s], lens[s] + 1, ... of their sequences.  pages [n_seqs, max_pages] and lens [n_seqs]: int32 on the device."""
     lib = _calls or load_library().by_address
     cu = _host_i32(cu_seqlens)
-    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
-    p, max_pages, n = _kv4_tables(pages, lens, cu.size - 1)
-    _on_current_device(k, v, k4, v4, k_scales, v_scales, pages, lens)
-    if k.shape != v.shape or tuple(k.shape[1:]) != (kvh, hd):
-        raise ValueError(f"k and v must be [total, {kvh}, {hd}]")
-    _check(lib.vfm_kv4_append(*_rows(k, "k"), *_rows(v, "v"), _i32_ptr(cu), cu.size - 1, k.shape[0], n, p, max_pages, *cache, kvh, hd,
-                              VFM_BF16, _stream_ptr(stream)))
+    n, here = cu.size - 1, _current_device()
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales, here)
+    table, max_pages = _kv4_pages(pages, here, n)
+    total = k.shape[0]
+    rows = (total, kvh, hd)
+    _check(lib.vfm_kv4_append(*_rows(k, "k", here, rows), *_rows(v, "v", here, rows), _i32_ptr(cu), n, total,
+                              _like(lens, "lens", here, (n,), _torch.int32), table, max_pages, *cache, kvh, hd, VFM_BF16, _stream_ptr(stream)))
 
 
 def vfm_kv4_gather(k4, v4, k_scales, v_scales, pages, cu_seqlens, k=None, v=None, stream=None) -> Tuple:
     """The first cu_seqlens[s+1] - cu_seqlens[s] places of every sequence as bf16 k, v [total, kv_heads, head_dim]."""
     lib = _calls or load_library().by_address
     cu = _host_i32(cu_seqlens)
-    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
-    p, max_pages, _ = _kv4_tables(pages, None, cu.size - 1)
-    _on_current_device(k4, v4, k_scales, v_scales, pages, k, v)
-    total = int(cu[-1])
+    n, here, bf16 = cu.size - 1, _current_device(), _torch.bfloat16
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales, here)
+    table, max_pages = _kv4_pages(pages, here, n)
+    total = int(cu[n])
+    rows = (total, kvh, hd)
     if k is None:
-        k = _torch.empty((total, kvh, hd), dtype=_torch.bfloat16, device=k4.device)
-        _used_on(stream, k)
+        k = _new(rows, bf16, k4, stream)
     if v is None:
-        v = _torch.empty((total, kvh, hd), dtype=_torch.bfloat16, device=k4.device)
-        _used_on(stream, v)
-    _check(lib.vfm_kv4_gather(*cache, p, max_pages, _i32_ptr(cu), cu.size - 1, total, kvh, hd,
-                              _like(k, "k", (total, kvh, hd), _torch.bfloat16), _like(v, "v", (total, kvh, hd), _torch.bfloat16),
-                              VFM_BF16, _stream_ptr(stream)))
+        v = _new(rows, bf16, k4, stream)
+    _check(lib.vfm_kv4_gather(*cache, table, max_pages, _i32_ptr(cu), n, total, kvh, hd, _like(k, "k", here, rows, bf16),
+                              _like(v, "v", here, rows, bf16), VFM_BF16, _stream_ptr(stream)))
     return k, v
 
 
@@ -634,21 +647,18 @@ def vfm_kv4_attn(q, k4, v4, k_scales, v_scales, pages, lens, cu_seqlens, scale: 
     lse [heads, total] (fp32)."""
     lib = _calls or load_library().by_address
     cu = _host_i32(cu_seqlens)
-    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales)
-    p, max_pages, n = _kv4_tables(pages, lens, cu.size - 1)
-    _on_current_device(q, k4, v4, k_scales, v_scales, pages, lens, out, lse, workspace)
-    if q.dim() != 3 or q.shape[2] != hd:
+    n, here = cu.size - 1, _current_device()
+    cache, kvh, hd = _kv4_cache(k4, v4, k_scales, v_scales, here)
+    table, max_pages = _kv4_pages(pages, here, n)
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != hd:
         raise ValueError(f"q must be [total, heads, {hd}]")
-    total, heads, _ = q.shape
-    if out is None:
-        out = _torch.empty((total, heads, hd), dtype=_torch.bfloat16, device=q.device)
-        _used_on(stream, out)
-    if lse is None:
-        lse = _torch.empty((heads, total), dtype=_torch.float32, device=q.device)
-        _used_on(stream, lse)
-    need = 0 if workspace is not None else int(lib.vfm_kv4_attn_workspace_size(_i32_ptr(cu), cu.size - 1, total, heads, kvh, hd))
-    ws, ws_bytes, keep = _workspace(workspace, need, q, stream)
-    _check(lib.vfm_kv4_attn(*_rows(q, "q"), *cache, p, max_pages, n, _i32_ptr(cu), cu.size - 1, total, heads, kvh, hd, float(scale),
-                            _like(out, "out", (total, heads, hd), _torch.bfloat16), _like(lse, "lse", (heads, total), _torch.float32),
-                            ws, ws_bytes, VFM_BF16, _stream_ptr(stream)))
+    total, heads, _ = shape
+    pq = _rows(q, "q", here, shape)
+    pn = _like(lens, "lens", here, (n,), _torch.int32)
+    cu_p = _i32_ptr(cu)
+    out, lse, po, pl = _out_lse(q, shape, out, lse, here, stream)
+    workspace, pw, nw = _workspace(workspace, lib.vfm_kv4_attn_workspace_size, (cu_p, n, total, heads, kvh, hd), q, here, stream)
+    _check(lib.vfm_kv4_attn(*pq, *cache, table, max_pages, pn, cu_p, n, total, heads, kvh, hd, scale, po, pl, pw, nw, VFM_BF16,
+                            _stream_ptr(stream)))
     return out, lse

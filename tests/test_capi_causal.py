@@ -140,7 +140,7 @@ def _dev(*shape, dtype=torch.bfloat16):
 
 
 def test_wrappers_refuse_what_the_kernels_would_misread(lib, monkeypatch):
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_current_device", lambda: 0)
     q, k = _dev(8, 4, 64), _dev(8, 2, 64)
     cu = [0, 8]
     out, lse = _dev(8, 4, 64), _dev(4, 8, dtype=torch.float32)
