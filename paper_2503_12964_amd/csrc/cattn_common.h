@@ -45,6 +45,13 @@ inline TileIndex make_causal_index(const XSegTable& segs, int group, int rows_pe
   return ti;
 }
 
+// The lane's number, formed where it is asked for: what is rarely needed takes no register in between.
+__device__ __forceinline__ int lane_anew() {
+  uint32_t zero = 0;
+  asm volatile("" : "+s"(zero));
+  return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, zero));
+}
+
 // store_tile_rows for rows that lie anywhere: dst(r) is the address of row r of the wavefront's tile (first column), asked
 // only for rows < rows_valid.
 template <int D, class Dst>
@@ -75,9 +82,6 @@ __device__ __forceinline__ void store_tile_rows_at(char* turn, const f32x16 (&ac
 
 hipError_t launch_cattn_fwd(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
                             int head_dim, void* out, float* lse, hipStream_t stream);
-// Delta and lse in log2 units of all rows of the call, and the sentinels.
-hipError_t launch_cattn_prepare(const void* out, const void* dout, const float* lse, float* delta, float* lse2,
-                                float* sentinel, int total_q, int n_heads, int head_dim, hipStream_t stream);
 hipError_t launch_cattn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
                             const void* dout, const XSegTable& segs, const CausalShape& sh, int head_dim,
                             void* dq, uint32_t dq_row, void* dk, uint32_t dk_row, void* dv, uint32_t dv_row,

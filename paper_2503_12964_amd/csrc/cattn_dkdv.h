@@ -1,0 +1,389 @@
+// dK, dV of causal attention with grouped heads: one workgroup owns 128 keys of one (sequence, K/V head), 32 per wavefront.
+// Included by cattn_bwd.hip.
+//
+// The loop is that of the bidirectional pass (bwd_dkdv_unit in attn_bwd.hip, where its choices are explained with
+// their measurements): row blocks of 32 in a software pipeline, S/dP products of block b+1 under the exponentials of block b,
+// tiles of 64 rows in a ring of three LDS stages requested two ahead, score products as assembly at head_dim 128 with K and V in
+// AGPRs.  What the causal order and the groups add:
+//  - A tile's rows are (query, head) pairs (cattn_common.h); a lane steps the addresses of its rows by 64 rows with one
+//    conditional correction, no division.
+//  - The walk begins at the tile of the first row that sees any of the keys, a wavefront's at the first that sees any of
+//    its own (in steps of the ring, so that every LDS address stays an immediate).
+//  - Scores of pairs that are not seen become -inf before their exponentials, in the blocks that cross the diagonal only.
+#pragma once
+
+#include "cattn_common.h"
+
+namespace vfm {
+
+constexpr int kCBwdWaves = 4;
+constexpr int kCBwdBC = 128;   // keys per workgroup
+constexpr int kCBwdBQ = 64;    // rows per LDS tile
+constexpr int kCBwdRing = 3;
+constexpr int kSgbValu = 0x002, kSgbMfma = 0x008, kSgbDsRead = 0x100;
+
+template <int D>
+struct CKvCfg {
+  static constexpr int kTileBytes = kCBwdBQ * D * 2;                     // one Q or dO tile
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kStatBytes = 4 * kCBwdBQ * 4;                     // lse2, Delta (+ spare) of one stage
+  static constexpr int kStatBase = kCBwdRing * kStageBytes;
+  static constexpr int kOwnK = 2 * kStageBytes;                          // K rows on their way: the ring's last stage
+  static constexpr int kOwnV = kStatBase + kCBwdRing * kStatBytes;       // V rows: behind the statistics
+  static constexpr int kLdsBytes = kOwnV + kCBwdBC * D * 2;
+  static_assert(kCBwdBC * D * 2 <= kStageBytes && kOwnV % 1024 == 0 && kLdsBytes <= 160 * 1024, "K rows fit a stage; LDS of one CU");
+  static constexpr int kChunksPerRow = D / 8;
+  static constexpr int kLoadsPerWave = kCBwdBQ * kChunksPerRow / (kCBwdWaves * 64);
+};
+
+template <int D>
+__global__ __launch_bounds__(kCBwdWaves * 64, D == 64 ? 2 : 1)
+void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                       const __bf16* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ delta,
+                       const float* __restrict__ sentinel, __bf16* __restrict__ dk, __bf16* __restrict__ dv,
+                       const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dk_row, uint32_t dv_row) {
+  using Cfg = CKvCfg<D>;
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int LPW = Cfg::kLoadsPerWave;
+  constexpr int SB = Cfg::kStageBytes;
+  constexpr int TB = Cfg::kTileBytes;
+  constexpr int RB = D * 2;
+  constexpr bool kAsm = D == 128;   // more than 256 registers (see mfma32_v)
+
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+
+  const int kvh = blockIdx.x % sh.n_kv_heads;
+  int seq, tk;
+  locate_tile(ti, segs.n, blockIdx.x / sh.n_kv_heads, seq, tk);   // a sequence's first keys, which most rows see, first
+  const CausalSeq cs = causal_seq(segs, seq, sh.group);
+  const int j0 = tk * kCBwdBC;
+
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63;
+  const int c = lane & 31;
+  const int g = lane >> 5;
+  const int jw = j0 + wave * 32;                       // the wavefront's first key
+  const int keys_valid = cs.kl - jw;
+  auto kv_row0 = [&](__bf16* base, uint32_t row_bytes) {
+    return reinterpret_cast<__bf16*>(reinterpret_cast<char*>(base) + (size_t)(cs.ks + jw) * row_bytes) + kvh * D;
+  };
+
+  // row that is the first to see key j
+  auto first_row = [&](int j) {
+    const long long r = ((long long)j - cs.off) * sh.group;
+    return r < 0 ? 0 : r > 0x7fffffffLL ? 0x7fffffff : (int)r;
+  };
+  const int rt0 = first_row(j0) / kCBwdBQ * kCBwdBQ;
+  const int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kCBwdBQ - 1) / kCBwdBQ : 0;
+  if (n_tiles == 0) {      // keys of a sequence without queries
+    if (c < keys_valid) {
+      const u32x2 z = {0u, 0u};
+#pragma unroll
+      for (int x = 0; x < D / 8; ++x) {
+        *reinterpret_cast<u32x2*>(kv_row0(dk, dk_row) + (size_t)c * (dk_row / 2) + 4 * g + 8 * x) = z;
+        *reinterpret_cast<u32x2*>(kv_row0(dv, dv_row) + (size_t)c * (dv_row / 2) + 4 * g + 8 * x) = z;
+      }
+    }
+    return;
+  }
+  const int row_min = first_row(jw + c);               // of this lane's key
+  const int wave_all = __builtin_amdgcn_readfirstlane(first_row(jw + 31));   // rows from here on see all of the wavefront's keys
+  // tiles whose rows see none of the wavefront's keys, in whole turns of the ring
+  int skip = __builtin_amdgcn_readfirstlane((first_row(jw) - rt0) / kCBwdBQ);
+  skip = (skip < n_tiles ? skip : n_tiles - 1) / kCBwdRing * kCBwdRing;
+
+  // ---- tile requests (direct global->LDS).  Lane L of wave instruction (x, wave) owns LDS chunk (x*waves + wave)*64 + L:
+  // row P / chunks_per_row, physical chunk P % chunks_per_row (the swizzle has a period of 16 rows, so the logical chunk
+  // does not depend on x).  Offsets count from the sequence's first query and step by 64 rows; past the last row
+  // they clamp to it.  Waves 0/2 fetch lse2, waves 1/3 Delta of the 64 rows (2 and 3 into spare LDS).
+  const uint32_t do_row = (uint32_t)sh.n_heads * RB;
+  const int d_tok = kCBwdBQ / sh.group, d_sub = kCBwdBQ - d_tok * sh.group;
+  const uint32_t q_step = (uint32_t)d_tok * sh.q_row + (uint32_t)d_sub * RB, q_wrap = sh.q_row - (uint32_t)sh.group * RB;
+  const uint32_t do_step = (uint32_t)d_tok * do_row + (uint32_t)d_sub * RB, do_wrap = do_row - (uint32_t)sh.group * RB;
+  const uint32_t q_last = (uint32_t)(cs.ql - 1) * sh.q_row + (uint32_t)(sh.group - 1) * RB;
+  const uint32_t do_last = (uint32_t)(cs.ql - 1) * do_row + (uint32_t)(sh.group - 1) * RB;
+  const char* qbase = uniform_ptr((const char*)q + (size_t)cs.qs * sh.q_row + (size_t)kvh * sh.group * RB);
+  const char* dobase = uniform_ptr((const char*)dout + ((size_t)cs.qs * sh.n_heads + (size_t)kvh * sh.group) * RB);
+  static_assert(kCBwdWaves * 64 / Cfg::kChunksPerRow % 16 == 0, "rows of consecutive x: whole periods of the swizzle apart");
+  uint32_t q_off[LPW], do_off[LPW];
+  int sub[LPW];
+  const int own_row = (wave * 64 + lane) / Cfg::kChunksPerRow;
+  const uint32_t colb = (uint32_t)(((lane % Cfg::kChunksPerRow) ^ swz<D>(own_row)) * 16);
+#pragma unroll
+  for (int x = 0; x < LPW; ++x) {
+    const int row = rt0 + x * (kCBwdWaves * 64 / Cfg::kChunksPerRow) + own_row, tok = row / sh.group;
+    sub[x] = row - tok * sh.group;
+    q_off[x] = (uint32_t)tok * sh.q_row + (uint32_t)sub[x] * RB;
+    do_off[x] = (uint32_t)tok * do_row + (uint32_t)sub[x] * RB;
+  }
+  const bool is_lse = (wave & 1) == 0;
+  const float* stat_src = uniform_ptr(is_lse ? lse2 : delta);
+  const uint32_t stat_sentinel = (uint32_t)((const char*)(sentinel + (is_lse ? 0 : 1)) - (const char*)stat_src);
+  int stat_row = rt0 + lane, stat_sub = stat_row % sh.group;
+  uint32_t stat_off = ((uint32_t)(kvh * sh.group + stat_sub) * sh.total_q + cs.qs + stat_row / sh.group) * 4u;
+  const uint32_t stat_step = ((uint32_t)d_sub * sh.total_q + d_tok) * 4u, stat_wrap = 4u - (uint32_t)sh.group * sh.total_q * 4u;
+  const uint32_t smem_addr = lds_addr_of(smem);
+  const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(smem_addr + wave * 1024);
+  const uint32_t stat_lds = __builtin_amdgcn_readfirstlane(smem_addr + Cfg::kStatBase + wave * (kCBwdBQ * 4));
+  auto issue_tile = [&](int stage) {
+#pragma unroll
+    for (int x = 0; x < LPW; ++x) {
+      const uint32_t dst = wave_lds + stage * SB + x * kCBwdWaves * 1024;
+      lds_dma16(qbase, min(q_off[x], q_last) + colb, dst);
+      lds_dma16(dobase, min(do_off[x], do_last) + colb, dst + TB);
+      sub[x] += d_sub;
+      const bool wrap = sub[x] >= sh.group;
+      q_off[x] += q_step + (wrap ? q_wrap : 0u);
+      do_off[x] += do_step + (wrap ? do_wrap : 0u);
+      sub[x] -= wrap ? sh.group : 0;
+    }
+    lds_dma4(stat_src, stat_row < cs.rows ? stat_off : stat_sentinel, stat_lds + stage * Cfg::kStatBytes);
+    stat_row += kCBwdBQ;
+    stat_sub += d_sub;
+    const bool wrap = stat_sub >= sh.group;
+    stat_off += stat_step + (wrap ? stat_wrap : 0u);
+    stat_sub -= wrap ? sh.group : 0;
+  };
+
+  // ---- per-lane LDS addresses within a tile (as in bwd_dkdv_unit): rows as A operand, transposing reads of the same rows
+  const int rbase = tile_off<D>(c, 8 * g);
+  int tbase[2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    tbase[t] = tile_off<D>(8 * t + 4 * g + ((lane & 15) >> 2), 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
+  constexpr int SETS = kCBwdRing * SB > 65536 ? 2 : 1;   // set 1: stage 2, beyond the 64 KB an immediate reaches
+  uint32_t rb[SETS][KS], tb[SETS][2][DB];
+#pragma unroll
+  for (int hs = 0; hs < SETS; ++hs) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      rb[hs][ks] = smem_addr + hs * 2 * SB + (rbase ^ (ks << 5));
+      asm volatile("" : "+v"(rb[hs][ks]));
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        tb[hs][t][db] = smem_addr + hs * 2 * SB + (tbase[t] ^ (db << 6));
+        asm volatile("" : "+v"(tb[hs][t][db]));
+      }
+  }
+
+  const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  f32x16 dkacc[DB], dvacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) { dkacc[db] = zero16; dvacc[db] = zero16; }
+
+  auto read_rows = [&](int stage, int ib, bf16x8 (&qa)[KS], bf16x8 (&da)[KS]) {
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const uint32_t a = rb[SETS == 2 ? stage >> 1 : 0][ks] + (SETS == 2 ? stage & 1 : stage) * SB + ib * 32 * RB;
+      qa[ks] = lds_read_b128_at(a);
+      da[ks] = lds_read_b128_at(a + TB);
+    }
+  };
+
+  // ---- prologue: K, V rows, tiles 0 and 1 requested
+  const uint32_t own = smem_addr + wave * (32 * RB);   // this wavefront's rows, from kOwnK and kOwnV on
+  {
+    const char* kbase = uniform_ptr((const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB);
+    const char* vbase = uniform_ptr((const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB);
+    const uint32_t own_s = __builtin_amdgcn_readfirstlane(own);
+#pragma unroll
+    for (int x = 0; x < 32 * RB / 1024; ++x) {
+      const int p = x * 64 + lane, r = p / Cfg::kChunksPerRow;
+      const uint32_t key = (uint32_t)min(jw + r, cs.kl - 1), col = (uint32_t)(((p % Cfg::kChunksPerRow) ^ swz<D>(r)) * 16);
+      lds_dma16(kbase, key * sh.k_row + col, own_s + Cfg::kOwnK + x * 1024);
+      lds_dma16(vbase, key * sh.v_row + col, own_s + Cfg::kOwnV + x * 1024);
+    }
+  }
+  issue_tile(0); issue_tile(1);
+  wait_vmcnt<0>();
+  bf16x8 kreg[KS], vreg[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    kreg[ks] = lds_read_b128_at(own + Cfg::kOwnK + (rbase ^ (ks << 5)));
+    vreg[ks] = lds_read_b128_at(own + Cfg::kOwnV + (rbase ^ (ks << 5)));
+    if constexpr (kAsm) { to_agpr(kreg[ks]); to_agpr(vreg[ks]); }
+    else { settle(kreg[ks]); settle(vreg[ks]); }
+  }
+  __syncthreads();
+
+  // tiles that the wavefront does not compute (none of its keys exist, or none is seen yet): its share of the requests, the
+  // waits and barriers
+  const int idle_tiles = keys_valid <= 0 ? n_tiles : skip;
+  for (int t = 0; t < idle_tiles; t += kCBwdRing) {
+#pragma unroll
+    for (int x = 0; x < kCBwdRing; ++x)
+      if (t + x < idle_tiles) {
+        wait_vmcnt<0>();
+        __syncthreads();
+        issue_tile((x + 2) % kCBwdRing);
+      }
+  }
+  if (keys_valid <= 0) {
+    wait_vmcnt<0>();
+    __syncthreads();
+    return;
+  }
+
+  bf16x8 qa_n[KS], da_n[KS];      // row operands of block b+1
+  f32x16 s_cur, dp_cur;           // S(b), dP(b)
+  {
+    bf16x8 q0r[KS], d0r[KS];
+    read_rows(0, 0, q0r, d0r);
+    read_rows(0, 1, qa_n, da_n);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if constexpr (kAsm) {
+        mfma32_v(s_cur, q0r[ks], kreg[ks], ks == 0);
+        mfma32_v(dp_cur, d0r[ks], vreg[ks], ks == 0);
+      } else {
+        s_cur = mfma32(q0r[ks], kreg[ks], ks == 0 ? zero16 : s_cur);
+        dp_cur = mfma32(d0r[ks], vreg[ks], ks == 0 ? zero16 : dp_cur);
+      }
+    }
+    if constexpr (kAsm) wait_mfma_v(s_cur, dp_cur);
+  }
+
+  // One pipeline iteration; POS = b % 6 fixes every LDS stage at compile time.  row0: first row of block b.
+  auto iteration = [&](auto pos_c, int row0) {
+    constexpr int POS = decltype(pos_c)::value;
+    constexpr int IB = POS & 1;                           // block b within its tile
+    constexpr int ST_CUR = (POS / 2) % kCBwdRing;         // stage of block b's tile
+    constexpr int ST_ROW = ((POS + 2) / 2) % kCBwdRing;   // stage of block b+2's tile
+    if constexpr (IB == 0) {
+      // Start of tile t = b/2: tile t+1 must have landed for every wave before anyone reads
+      // block b+2's rows, and every wave is past tile t-1, whose stage takes tile t+2.
+      wait_vmcnt<0>();
+      __syncthreads();
+      issue_tile((ST_CUR + 2) % kCBwdRing);
+    }
+    if (row0 < wave_all) {   // (wave-uniform) the block crosses the diagonal: rows that do not see this lane's key
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (row0 + 8 * (e >> 2) + 4 * g + (e & 3) < row_min) s_cur[e] = -INFINITY;
+    }
+    const float* lse_s = reinterpret_cast<const float*>(smem + Cfg::kStatBase + ST_CUR * Cfg::kStatBytes);
+    const float* delta_s = lse_s + kCBwdBQ;              // wave 1's statistics follow wave 0's
+
+    // ---- phase A: S(b+1), dP(b+1) | P(b) | statistics and transposed-operand reads of block b (one group per product)
+    constexpr int NG = 2 * KS;
+    f32x4 l4[4], d4[4];
+    s16x4 dlo[2][DB], dhi[2][DB], qlo[2][DB], qhi[2][DB];
+    f32x16 s_next, dp_next, p;
+    u32x8 pw;
+#pragma unroll
+    for (int gi = 0; gi < NG; ++gi) {
+      const int ks = gi >> 1;
+      if constexpr (kAsm) {
+        if ((gi & 1) == 0) mfma32_v(s_next, qa_n[ks], kreg[ks], ks == 0, s_cur, p, pw);
+        else mfma32_v(dp_next, da_n[ks], vreg[ks], ks == 0, s_cur, p, pw);
+      } else {
+        if ((gi & 1) == 0) s_next = mfma32(qa_n[ks], kreg[ks], ks == 0 ? zero16 : s_next);
+        else dp_next = mfma32(da_n[ks], vreg[ks], ks == 0 ? zero16 : dp_next);
+      }
+      if (gi == 0) {
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) l4[q4] = *reinterpret_cast<const f32x4*>(lse_s + IB * 32 + 8 * q4 + 4 * g);
+      }
+#pragma unroll
+      for (int r = 2 * gi; r < 2 * gi + 2; ++r) {
+        const int rr = r % (4 * DB), s2 = rr / (2 * DB), db = (rr >> 1) % DB, hi = rr & 1;
+        const uint32_t o = tb[SETS == 2 ? ST_CUR >> 1 : 0][hi][db] + (SETS == 2 ? ST_CUR & 1 : ST_CUR) * SB + (IB * 32 + 16 * s2) * RB;
+        if (r < 4 * DB) { if (hi) dhi[s2][db] = lds_read_tr_at(o + TB); else dlo[s2][db] = lds_read_tr_at(o + TB); }
+        else { if (hi) qhi[s2][db] = lds_read_tr_at(o); else qlo[s2][db] = lds_read_tr_at(o); }
+      }
+      if (gi >= NG - 2) {
+#pragma unroll
+        for (int q4 = 2 * (gi - (NG - 2)); q4 < 2 * (gi - (NG - 2)) + 2; ++q4)
+          d4[q4] = *reinterpret_cast<const f32x4*>(delta_s + IB * 32 + 8 * q4 + 4 * g);
+      }
+      // P for rows 8*(e/4) + 4g + e%4 of the block, column = this lane's key; a pair is converted one group after its
+      // exponentials
+#pragma unroll
+      for (int e = 1; e < 16; e += 2)
+        if (e * (NG - 2) / 16 + 3 == gi) {
+          const f32x2 pr = {p[e - 1], p[e]};
+          pw[e >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+        }
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e * (NG - 2) / 16 + 2 == gi) p[e] = fast_exp2(s_cur[e] * sh.scale_log2 - l4[e >> 2][e & 3]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    {
+      const f32x2 pr = {p[14], p[15]};   // the last pair's group would be NG
+      pw[7] = __builtin_bit_cast(uint32_t, __builtin_convertvector(pr, bf16x2));
+    }
+    bf16x8 pb[2];
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      const u32x4 w = {pw[4 * s2], pw[4 * s2 + 1], pw[4 * s2 + 2], pw[4 * s2 + 3]};
+      pb[s2] = __builtin_bit_cast(bf16x8, w);
+    }
+
+    // ---- phase B: dV^T += dO(b)^T P(b) | dS(b) = P(b) o (dP(b) - Delta)
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        dvacc[db] = mfma32(join_tr(dlo[s2][db], dhi[s2][db]), pb[s2], dvacc[db]);
+    bf16x8 dsb[2];
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2) {
+      f32x8 a;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int r = 8 * s2 + e;
+        a[e] = p[r] * (dp_cur[r] - d4[r >> 2][r & 3]);
+      }
+      dsb[s2] = to_bf16x8(a);
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSgbMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgbValu, 5, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- phase C: dK^T += Q(b)^T dS(b) | row operands of block b+2
+#pragma unroll
+    for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        dkacc[db] = mfma32(join_tr(qlo[s2][db], qhi[s2][db]), dsb[s2], dkacc[db]);
+    bf16x8 qa_2[KS], da_2[KS];
+    read_rows(ST_ROW, IB, qa_2, da_2);
+#pragma unroll
+    for (int i = 0; i < 2 * DB; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kSgbMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kSgbDsRead, (2 * KS + 2 * DB - 1) / (2 * DB), 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    s_cur = s_next;
+    dp_cur = dp_next;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) { qa_n[ks] = qa_2[ks]; da_n[ks] = da_2[ks]; }
+  };
+
+  static_assert(kCBwdRing == 3, "the block loop is unrolled over the ring");
+  for (int t = skip; t < n_tiles; t += 3) {
+    const int row = rt0 + t * kCBwdBQ;
+    iteration(IntC<0>{}, row);
+    iteration(IntC<1>{}, row + 32);
+    if (t + 1 < n_tiles) { iteration(IntC<2>{}, row + 64); iteration(IntC<3>{}, row + 96); }
+    if (t + 2 < n_tiles) { iteration(IntC<4>{}, row + 128); iteration(IntC<5>{}, row + 160); }
+  }
+  wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
+
+  // ---- epilogue: dK (scaled) and dV of this wavefront's keys
+  __syncthreads();   // the ring is free: each wavefront turns its tiles through a piece of it
+  char* turn = smem + wave * (32 * RB);
+  store_tile_rows<D>(turn, dkacc, sh.scale, kv_row0(dk, dk_row), dk_row / 2, keys_valid);
+  store_tile_rows<D>(turn, dvacc, 1.0f, kv_row0(dv, dv_row), dv_row / 2, keys_valid);
+}
+
+}  // namespace vfm

@@ -64,10 +64,7 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   const int row_w = r0 + wave * 32;                             // the wavefront's first row
   const int rows_valid = cs.rows - row_w;                       // may be <= 0, or more than 32
   auto row_tok = [&](int r) { return r / sh.group; };
-  const int my_row = min(row_w + c, cs.rows - 1);
-  const int my_tok = row_tok(my_row);
-  const int my_head = kvh * sh.group + (my_row - my_tok * sh.group);
-  const int lim = my_tok + cs.off;                              // this lane's row sees keys <= lim
+  const int lim_g = row_tok(min(row_w + c, cs.rows - 1)) + cs.off - 4 * g;   // this lane's row sees keys <= lim_g + 4 g
   // keys that the tile, and this wavefront, look at
   const int n_keys = row_tok(min(r0 + Cfg::kRows, cs.rows) - 1) + cs.off + 1;
   const int n_units = n_keys > 0 ? (n_keys + kCU - 1) / kCU : 0;
@@ -80,8 +77,12 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
     const int row = row_w + r, tok = row_tok(row);
     return out + ((size_t)(cs.qs + tok) * sh.n_heads + kvh * sh.group + (row - tok * sh.group)) * D;
   };
+  auto lse_at = [&](int row) {
+    const int tok = row_tok(row);
+    return (size_t)(kvh * sh.group + (row - tok * sh.group)) * sh.total_q + cs.qs + tok;
+  };
   auto write_empty = [&]() {                                    // rows that see no key
-    if (row_w + c < cs.rows && g == 0) lse[(size_t)my_head * sh.total_q + cs.qs + my_tok] = -INFINITY;
+    if (row_w + c < cs.rows && g == 0) lse[lse_at(row_w + c)] = -INFINITY;
     const u32x4 z = {0u, 0u, 0u, 0u};
     for (int i = lane; i < 32 * Cfg::kChunksPerRow; i += 64) {
       const int r = i / Cfg::kChunksPerRow;
@@ -162,7 +163,7 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
     if (j0 + kCU - 1 > wave_min) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (j0 + 8 * (r >> 2) + 4 * g + (r & 3) > lim) s[r] = -INFINITY;
+        if (j0 + 8 * (r >> 2) + (r & 3) > lim_g) s[r] = -INFINITY;
     }
   };
 
@@ -345,8 +346,8 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   // ---- epilogue: normalise, write out (bf16) and lse (natural log); a row without keys: 0 and -inf
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
-  if (row_w + c < cs.rows && g == 0)
-    lse[(size_t)my_head * sh.total_q + cs.qs + my_tok] = lim < 0 ? -INFINITY : (m_run + __log2f(l_tot)) * kCLn2;
+  const int row = row_w + (lane_anew() & 31);
+  if (row < cs.rows && lane_anew() < 32) lse[lse_at(row)] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kCLn2;
   __syncthreads();   // the rings are free: each wavefront turns its tile through a piece of them
   store_tile_rows_at<D>(smem + wave * (32 * RB), oacc, inv, rows_valid, out_row);
 }

@@ -186,10 +186,6 @@ int vfm_cattn_bwd(const void* q, int64_t q_stride, const void* k, int64_t k_stri
   float* sentinel = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * part);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const CausalShape sh = make_shape(total_q, n_heads, n_kv_heads, q_stride, k_stride, v_stride, scale);
-  if (total_q > 0) {
-    hipError_t e = vfm::launch_cattn_prepare(out, dout, lse, delta, lse2, sentinel, total_q, n_heads, head_dim, stream);
-    if (e != hipSuccess) return vfm::launch_status(e);
-  }
   for (int s0 = 0; s0 < n_seqs; s0 += VFM_MAX_XSEQS) {
     XSegTable segs;
     build_table(cu_seqlens_q + s0, cu_seqlens_kv + s0, std::min(VFM_MAX_XSEQS, n_seqs - s0), &segs);
