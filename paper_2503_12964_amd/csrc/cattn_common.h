@@ -45,6 +45,22 @@ inline TileIndex make_causal_index(const XSegTable& segs, int group, int rows_pe
   return ti;
 }
 
+// locate_tile for a whole wavefront that asks for one tile: every lane looks at the boundaries that it holds, one round of loads
+// where the binary search takes a dependent one per step.  cu has `room` + 1 entries, those past n repeating the total or unused.
+template <int ROOM>
+__device__ __forceinline__ void locate_tile_wave(const int* cu, int n, int tile, int& s, int& t) {
+  const int lane = threadIdx.x & 63;
+  int below = 0;
+#pragma unroll
+  for (int x = 0; x < ROOM; x += 64) {
+    const int i = x + lane;
+    const bool le = i < n && cu[i < n ? i : 0] <= tile;
+    below += __builtin_popcountll(__builtin_amdgcn_ballot_w64(le));
+  }
+  s = __builtin_amdgcn_readfirstlane(below - 1);     // the last sequence that begins at or before it
+  t = tile - cu[s];
+}
+
 // The lane's number, formed where it is asked for: what is rarely needed takes no register in between.
 __device__ __forceinline__ int lane_anew() {
   uint32_t zero = 0;
@@ -81,7 +97,8 @@ __device__ __forceinline__ void store_tile_rows_at(char* turn, const f32x16 (&ac
 }
 
 hipError_t launch_cattn_fwd(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
-                            int head_dim, void* out, float* lse, hipStream_t stream);
+                            int head_dim, void* out, float* lse, void* workspace, hipStream_t stream);
+size_t cattn_fwd_workspace(const XSegTable& segs, const CausalShape& sh, int head_dim);   // bytes that the run needs
 hipError_t launch_cattn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
                             const void* dout, const XSegTable& segs, const CausalShape& sh, int head_dim,
                             void* dq, uint32_t dq_row, void* dk, uint32_t dk_row, void* dv, uint32_t dv_row,

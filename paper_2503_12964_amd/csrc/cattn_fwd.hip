@@ -9,6 +9,8 @@
 // a unit's exponentials would grow too large, K and V in rings of four LDS slots.  What the causal order adds: a wavefront masks only the
 // units that reach past its first row's limit, computes none past its last row's (it keeps fetching its share and
 // meeting the barriers for the wavefronts behind it), and row tiles are handed out longest first.
+#include <math.h>
+
 #include "cattn_common.h"
 
 namespace vfm {
@@ -17,6 +19,7 @@ constexpr int kCU = 32;                 // keys per pipeline unit
 constexpr int kCRing = 4;               // LDS ring slots for K and for V
 constexpr float kCLog2e = 1.4426950408889634f;
 constexpr float kCLn2 = 0.6931471805599453f;
+constexpr float kCUnset = -3.0e38f;      // reference of a row that has seen no key
 constexpr float kCSafeSum = 256.0f;     // a unit's exponentials may sum to this before the reference moves
 
 template <int D, int W>
@@ -24,19 +27,28 @@ struct CFwdCfg {
   static constexpr int kRows = W * 32;
   static constexpr int kUnitBytes = kCU * D * 2;
   static constexpr int kQBase = (2 * kCRing - 2) * kUnitBytes;     // Q rows: over the V ring's last two slots and behind
-  static constexpr int kLdsBytes = kQBase + kRows * D * 2;
-  static_assert(kRows * D * 2 >= 2 * kUnitBytes && kLdsBytes <= 160 * 1024, "rings, LDS of one CU");
+  static constexpr int kLdsBytes = kQBase + (kRows * D * 2 > 2 * kUnitBytes ? kRows * D * 2 : 2 * kUnitBytes);
+  static_assert(kLdsBytes <= 160 * 1024, "LDS of one CU");
   static constexpr int kChunksPerRow = D / 8;
   static constexpr int kLoadsPerWave = kCU * kChunksPerRow / (W * 64);
 };
 
 constexpr int kSgcValu = 0x002, kSgcMfma = 0x008, kSgcDsRead = 0x100;
 
+// Wavefronts per SIMD
+constexpr int fwd_waves(int D, int W) { return W == 1 ? 1 : W == 2 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
+
+// What a workgroup does of one tile: the units [u0, u1) of the keys that the tile's last row sees.  slot: null, or where the
+// unfinished results of a tile go that other workgroups share: per wavefront its accumulators as they lie (16 bytes a
+// lane), then the reference and the sum of its 32 rows.
 template <int D, int W>
-__global__ __launch_bounds__(W * 64, D == 64 ? 3 : 2)
-void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
-                      __bf16* __restrict__ out, float* __restrict__ lse, const XSegTable segs, const TileIndex ti,
-                      const CausalShape sh) {
+constexpr size_t slot_floats() { return (size_t)W * (32 * D + 64); }
+
+template <int D, int W, class Segs>
+__device__ __forceinline__
+void fwd_segment(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                 __bf16* __restrict__ out, float* __restrict__ lse, const Segs& segs, const CausalShape& sh, int kvh, int seq,
+                 int tq, int u0, int u1, float* __restrict__ slot) {
   using Cfg = CFwdCfg<D, W>;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int LPW = Cfg::kLoadsPerWave;
@@ -45,19 +57,11 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   constexpr int kInFlight = 2 * 2 * LPW;
 
   extern __shared__ __attribute__((aligned(16))) char smem[];
-
-  // workgroup b: all K/V heads of one tile before the next (heads on consecutive XCDs: an XCD keeps to its heads), a
-  // sequence's last tile, which sees most, first
-  const int kvh = blockIdx.x % sh.n_kv_heads;
-  int seq, tq;
-  locate_tile(ti, segs.n, blockIdx.x / sh.n_kv_heads, seq, tq);
   const CausalSeq cs = causal_seq(segs, seq, sh.group);
-  tq = (cs.rows + Cfg::kRows - 1) / Cfg::kRows - 1 - tq;
   const int r0 = tq * Cfg::kRows;                               // first row of the tile
 
-  const int tid = threadIdx.x;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = lane_anew();         // (what hangs on it is not carried from one segment to the next)
   const int c = lane & 31;
   const int g = lane >> 5;
 
@@ -65,12 +69,12 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   const int rows_valid = cs.rows - row_w;                       // may be <= 0, or more than 32
   auto row_tok = [&](int r) { return r / sh.group; };
   const int lim_g = row_tok(min(row_w + c, cs.rows - 1)) + cs.off - 4 * g;   // this lane's row sees keys <= lim_g + 4 g
-  // keys that the tile, and this wavefront, look at
-  const int n_keys = row_tok(min(r0 + Cfg::kRows, cs.rows) - 1) + cs.off + 1;
-  const int n_units = n_keys > 0 ? (n_keys + kCU - 1) / kCU : 0;
+  // units that the workgroup, and this wavefront, look at, counted from u0
+  const int n_units = u1 - u0;
   const int wave_min = __builtin_amdgcn_readfirstlane(row_tok(min(row_w, cs.rows - 1)) + cs.off);   // its first row's limit
   const int wave_last = row_tok(min(row_w + 32, cs.rows) - 1) + cs.off;
-  const int wave_units = __builtin_amdgcn_readfirstlane(rows_valid <= 0 || wave_last < 0 ? 0 : wave_last / kCU + 1);
+  const int wave_units = __builtin_amdgcn_readfirstlane(
+      rows_valid <= 0 || wave_last < u0 * kCU ? 0 : min(wave_last / kCU + 1 - u0, n_units));
 
   // address of row r of the wavefront's tile in out
   auto out_row = [&](int r) {
@@ -81,7 +85,17 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
     const int tok = row_tok(row);
     return (size_t)(kvh * sh.group + (row - tok * sh.group)) * sh.total_q + cs.qs + tok;
   };
-  auto write_empty = [&]() {                                    // rows that see no key
+  float* const wave_slot = slot + wave * (32 * D + 64);
+  auto write_empty = [&]() {                                    // rows that see no key of these
+    if (slot) {
+      if (rows_valid <= 0) return;
+      if (lane < 32) {
+        wave_slot[32 * D + 2 * lane] = kCUnset;
+        wave_slot[32 * D + 2 * lane + 1] = 0.f;
+      }
+      for (int i = lane; i < 8 * D; i += 64) reinterpret_cast<f32x4*>(wave_slot)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      return;
+    }
     if (row_w + c < cs.rows && g == 0) lse[lse_at(row_w + c)] = -INFINITY;
     const u32x4 z = {0u, 0u, 0u, 0u};
     for (int i = lane; i < 32 * Cfg::kChunksPerRow; i += 64) {
@@ -101,8 +115,8 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   for (int x = 0; x < LPW; ++x) {
     const int p = (x * W + wave) * 64 + lane;
     const int r = p / Cfg::kChunksPerRow;
-    k_rowoff[x] = (uint32_t)r * sh.k_row;
-    v_rowoff[x] = (uint32_t)r * sh.v_row;
+    k_rowoff[x] = (uint32_t)(u0 * kCU + r) * sh.k_row;
+    v_rowoff[x] = (uint32_t)(u0 * kCU + r) * sh.v_row;
     st_colb[x] = (uint32_t)(((p % Cfg::kChunksPerRow) ^ swz<D>(r)) * 16);
   }
   const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(lds_addr_of(smem) + wave * 1024);
@@ -159,7 +173,7 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
     for (int ks = 0; ks < KS; ++ks) ka[ks] = lds_read_b128(kt, kbase_off ^ (ks << 5));
   };
   auto mask = [&](int u, f32x16& s) {    // keys that the lane's row does not see
-    const int j0 = u * kCU;
+    const int j0 = (u0 + u) * kCU;
     if (j0 + kCU - 1 > wave_min) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
@@ -201,14 +215,15 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
     for (int ks = 0; ks < KS; ++ks) s_cur = mfma32(k0[ks], qreg[ks], ks == 0 ? zero16 : s_cur);
     mask(0, s_cur);
   }
-  // first reference point: the row maximum of unit 0 (a row that sees any key sees key 0); 0 for a row that sees none
+  // first reference point: the row maximum of the first unit (a row that sees any of these keys sees the first); a row that sees
+  // none keeps a finite one, far below all others
   float m_run, l_run = 0.f;
   {
     float mx = s_cur[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s_cur[r]);
     m_run = pair_max(mx) * sh.scale_log2;
-    if (m_run == -INFINITY) m_run = 0.f;
+    if (m_run == -INFINITY) m_run = kCUnset;
   }
   __syncthreads();            // every wave holds K(0), K(1) in registers: slots 0, 1 are free
   issue_k(0);                 // K unit 4
@@ -343,6 +358,24 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   for (int u = wave_units; u < n_units; ++u) idle_unit(u);
   wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
 
+  if (slot) {
+    float* o = slot + wave * (32 * D + 64);
+    const int ln = lane_anew();
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        reinterpret_cast<f32x4*>(o)[(db * 4 + q4) * 64 + ln] =
+            f32x4{oacc[db][q4 * 4], oacc[db][q4 * 4 + 1], oacc[db][q4 * 4 + 2], oacc[db][q4 * 4 + 3]};
+    const float l_part = pair_sum(l_run);
+    if (ln < 32) {
+      o[32 * D + 2 * ln] = m_run;
+      o[32 * D + 2 * ln + 1] = l_part;
+    }
+    __syncthreads();
+    return;
+  }
+
   // ---- epilogue: normalise, write out (bf16) and lse (natural log); a row without keys: 0 and -inf
   const float l_tot = pair_sum(l_run);
   const float inv = l_tot == 0.f ? 0.f : 1.0f / l_tot;
@@ -352,27 +385,293 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   store_tile_rows_at<D>(smem + wave * (32 * RB), oacc, inv, rows_valid, out_row);
 }
 
+// Units of the keys that the last row of tile tq sees
+__host__ __device__ inline int tile_units(int rows, int off, int group, int rows_per_tile, int tq) {
+  const int last = ((tq + 1) * rows_per_tile < rows ? (tq + 1) * rows_per_tile : rows) - 1;
+  const int keys = last / group + off + 1;
+  return keys > 0 ? (keys + kCU - 1) / kCU : 0;
+}
+
+// One workgroup per (K/V head, tile): all K/V heads of one tile before the next (heads on consecutive XCDs: an XCD keeps to
+// its heads), a sequence's last tile, which sees most, first.
 template <int D, int W>
-static hipError_t launch_cfg(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
-                             void* out, float* lse, hipStream_t stream) {
+__global__ __launch_bounds__(W * 64, fwd_waves(D, W))
+void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                      __bf16* __restrict__ out, float* __restrict__ lse, const XSegTable segs, const TileIndex ti,
+                      const CausalShape sh) {
+  constexpr int kRows = W * 32;
+  const int kvh = blockIdx.x % sh.n_kv_heads;
+  int seq, t;
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads, seq, t);
+  const CausalSeq cs = causal_seq(segs, seq, sh.group);
+  const int tq = (cs.rows + kRows - 1) / kRows - 1 - t;
+  fwd_segment<D, W>(q, k, v, out, lse, segs, sh, kvh, seq, tq, 0, tile_units(cs.rows, cs.off, sh.group, kRows, tq), nullptr);
+}
+
+// ---------------------------------------------------------------- few tiles, many keys
+// A chunk of a prompt against a long past is fewer tiles than the chip has CUs, and each takes as long as the past is long.
+// Then every K/V head's line of units (tile after tile) is cut into equal pieces, one workgroup each.  A tile within a piece
+// is finished there; a cut tile's parts go to the workspace, and a second launch joins them in order.
+constexpr int kSplitSeqs = 32;          // the plan travels in 4 KB of kernel arguments
+constexpr int kSplitPieces = 768;
+constexpr int kSplitTile = 5;           // a tile's prologue and epilogue, as units
+constexpr int kSplitJoin = 10;          // the second launch, as units
+
+struct SplitPlan {
+  int n, pieces;
+  int qs[kSplitSeqs], ql[kSplitSeqs], ks[kSplitSeqs], kl[kSplitSeqs];
+  int cu[kSplitSeqs + 1];               // tiles of the sequences before
+  uint32_t start[kSplitPieces + 1];     // (tile << 16 | unit) where a piece begins; the last: where all end
+  __device__ __host__ int q_start(int s) const { return qs[s]; }
+  __device__ __host__ int q_len(int s) const { return ql[s]; }
+  __device__ __host__ int kv_start(int s) const { return ks[s]; }
+  __device__ __host__ int kv_len(int s) const { return kl[s]; }
+};
+
+// Cuts a run into pieces if that pays; false: it does not (or the plan cannot hold it).  In units (0.45 us with 128 rows, which
+// one workgroup per CU does at the chip's full rate): without, the run takes as long as its longest tile.  In pieces it takes work
+// / pieces and the traffic of the cuts, rows * head_dim * 8 bytes each out and back, which all pieces make at once: with as many
+// pieces as there is room (rows * head_dim / 2048 + 2) units per end of a piece.
+static bool make_split(const XSegTable& segs, const CausalShape& sh, int rows_per_tile, int head_dim, int slots, SplitPlan* plan) {
+  if (segs.n > kSplitSeqs || segs.n == 0) return false;
+  long long cost = 0;
+  int tiles = 0, longest = 0;
+  for (int s = 0; s < segs.n; ++s) {
+    const long long rows = (long long)segs.ql[s] * sh.group, n = (rows + rows_per_tile - 1) / rows_per_tile;
+    if (tiles + n > 0xffff || (tiles + n) * sh.n_kv_heads > 2LL * slots) return false;   // (enough of them)
+    for (int t = 0; t < n; ++t) {
+      const int u = tile_units((int)rows, segs.kl[s] - segs.ql[s], sh.group, rows_per_tile, t);
+      if (u > longest) longest = u;
+      cost += u + kSplitTile;
+    }
+    tiles += (int)n;
+  }
+  const int room = slots / sh.n_kv_heads < kSplitPieces ? slots / sh.n_kv_heads : kSplitPieces;
+  if (room < 2 || longest > 0xffff) return false;
+  const float ends = 2.f * (rows_per_tile * head_dim / 2048 + 2);
+  int pieces = (int)sqrtf((float)cost * room / ends);          // where work / pieces + ends * pieces / room is least
+  if (pieces > room) pieces = room;
+  if (pieces < 2 || (float)cost / pieces + ends * pieces / room + kSplitJoin > 0.8f * (longest + kSplitTile)) return false;
+  plan->n = segs.n;
+  int at = 0;
+  for (int s = 0; s <= kSplitSeqs; ++s) {
+    plan->cu[s] = at;
+    if (s == kSplitSeqs) break;
+    const bool live = s < segs.n;
+    plan->qs[s] = live ? segs.qs[s] : 0;
+    plan->ql[s] = live ? segs.ql[s] : 0;
+    plan->ks[s] = live ? segs.ks[s] : 0;
+    plan->kl[s] = live ? segs.kl[s] : 0;
+    if (live) at += (int)(((long long)segs.ql[s] * sh.group + rows_per_tile - 1) / rows_per_tile);
+  }
+  int p = 0;
+  long long before = 0;
+  plan->start[p++] = 0;
+  for (int s = 0, tile = 0; s < segs.n; ++s) {
+    const int rows = segs.ql[s] * sh.group, n = (rows + rows_per_tile - 1) / rows_per_tile;
+    for (int t = 0; t < n; ++t, ++tile) {
+      const int u = tile_units(rows, segs.kl[s] - segs.ql[s], sh.group, rows_per_tile, n - 1 - t);
+      for (; p < pieces; ++p) {
+        long long cut = cost * p / pieces - before - kSplitTile;   // in units of this tile
+        if (cut >= u - 2) break;                                   // (a part of one or two units is not worth its slot)
+        if (cut < 2) cut = 0;
+        const uint32_t at = (uint32_t)tile << 16 | (uint32_t)cut;
+        if (at <= plan->start[p - 1]) { plan->start[p] = plan->start[p - 1]; continue; }   // an empty piece
+        plan->start[p] = at;
+      }
+      before += u + kSplitTile;
+    }
+  }
+  for (; p <= pieces; ++p) plan->start[p] = (uint32_t)tiles << 16;
+  plan->pieces = pieces;
+  return true;
+}
+
+__device__ __forceinline__ void split_tile(const SplitPlan& plan, const CausalShape& sh, int rows_per_tile, int tile, int& seq, int& tq, int& units) {
+  int t;
+  locate_tile_wave<kSplitSeqs>(plan.cu, plan.n, tile, seq, t);
+  const CausalSeq cs = causal_seq(plan, seq, sh.group);
+  tq = (cs.rows + rows_per_tile - 1) / rows_per_tile - 1 - t;
+  units = tile_units(cs.rows, cs.off, sh.group, rows_per_tile, tq);
+}
+
+template <int D, int W>
+__global__ __launch_bounds__(W * 64, fwd_waves(D, W))
+void cattn_fwd_split_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
+                            __bf16* __restrict__ out, float* __restrict__ lse, const SplitPlan plan, const CausalShape sh,
+                            float* __restrict__ slots) {
+  const int kvh = blockIdx.x % sh.n_kv_heads, piece = blockIdx.x / sh.n_kv_heads;
+  const uint32_t from = plan.start[piece], to = plan.start[piece + 1];
+  int tile = from >> 16, u = from & 0xffff;
+  for (bool first = true; (((uint32_t)tile << 16) | (uint32_t)u) < to; first = false) {
+    int seq, tq, units;
+    split_tile(plan, sh, W * 32, tile, seq, tq, units);
+    const int end = tile < (int)(to >> 16) ? units : (int)(to & 0xffff);
+    float* slot = u == 0 && end == units ? nullptr : slots + (size_t)(2 * blockIdx.x + (first ? 0 : 1)) * slot_floats<D, W>();
+    if (!first) __syncthreads();
+    fwd_segment<D, W>(q, k, v, out, lse, plan, sh, kvh, seq, tq, u, end, slot);
+    ++tile;
+    u = 0;
+  }
+}
+
+// Joins the parts of the tile that piece boundary blockIdx.x + 1 cuts, if no earlier boundary cuts it.  Workgroup y of a tile
+// takes 32 of its rows, a wavefront 32 columns of them and every fourth part, four of those at a time; the four shares
+// are then summed in order.
+constexpr int kJoinShares = 4;
+template <int D, int W>
+__global__ __launch_bounds__(D * 2 * kJoinShares)
+void cattn_fwd_join_kernel(__bf16* __restrict__ out, float* __restrict__ lse, const SplitPlan plan, const CausalShape sh,
+                           const float* __restrict__ slots) {
+  const int kvh = blockIdx.x % sh.n_kv_heads, p = blockIdx.x / sh.n_kv_heads + 1;
+  const uint32_t at = plan.start[p], prev = plan.start[p - 1];
+  const int tile = at >> 16;
+  if ((at & 0xffff) == 0 || at == prev) return;
+  if ((int)(prev >> 16) == tile && (prev & 0xffff) != 0) return;
+  int seq, tq, units;
+  split_tile(plan, sh, W * 32, tile, seq, tq, units);
+  const CausalSeq cs = causal_seq(plan, seq, sh.group);
+  __shared__ __attribute__((aligned(16))) float shares[(kJoinShares - 1) * (D / 32)][18][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), db = wave % (D / 32), share = wave / (D / 32), lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
+  const int row_w = tq * W * 32 + blockIdx.y * 32;
+  if (row_w >= cs.rows) return;
+  // the tile's parts: pieces p - 1 .. last (empty pieces among them have none)
+  int last = p;
+  while (last + 1 < plan.pieces && (int)(plan.start[last + 1] >> 16) == tile) ++last;
+  auto part = [&](int x) {
+    // the tile is the first segment of every piece but the one that it begins within
+    const bool later = x == p - 1 && prev < ((uint32_t)tile << 16);
+    return slots + (size_t)(2 * (x * sh.n_kv_heads + kvh) + (later ? 1 : 0)) * slot_floats<D, W>() + blockIdx.y * (32 * D + 64);
+  };
+  float o[16], m = kCUnset, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) o[i] = 0.f;
+  constexpr int kAtOnce = 4;
+  for (int x0 = p - 1 + share; x0 <= last; x0 += kAtOnce * kJoinShares) {
+    float pm[kAtOnce], pl[kAtOnce];
+    f32x4 v[kAtOnce][4];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int x = x0 + i * kJoinShares;
+      const bool there = x <= last && plan.start[x < plan.pieces ? x : 0] != plan.start[x < plan.pieces ? x + 1 : 0];
+      pm[i] = kCUnset;
+      pl[i] = 0.f;
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) v[i][q4] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (there) {
+        const float* s = part(x);
+        pm[i] = s[32 * D + 2 * c];
+        pl[i] = s[32 * D + 2 * c + 1];
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) v[i][q4] = reinterpret_cast<const f32x4*>(s)[(db * 4 + q4) * 64 + lane];
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) mn = fmaxf(mn, pm[i]);
+    const float a = fast_exp2(m - mn);
+    m = mn;
+    l *= a;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] *= a;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float b = fast_exp2(pm[i] - mn);
+      l += pl[i] * b;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[e] += v[i][e >> 2][e & 3] * b;
+    }
+  }
+  if (share > 0) {
+    float (*mine)[64] = shares[(share - 1) * (D / 32) + db];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mine[i][lane] = o[i];
+    mine[16][lane] = m;
+    mine[17][lane] = l;
+  }
+  __syncthreads();
+  if (share > 0 || row_w + c >= cs.rows) return;
+#pragma unroll
+  for (int x = 0; x < kJoinShares - 1; ++x) {
+    const float (*other)[64] = shares[x * (D / 32) + db];
+    const float mn = fmaxf(m, other[16][lane]), a = fast_exp2(m - mn), b = fast_exp2(other[16][lane] - mn);
+    m = mn;
+    l = l * a + other[17][lane] * b;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[i] = o[i] * a + other[i][lane] * b;
+  }
+  const int row = row_w + c, tok = row / sh.group, head = kvh * sh.group + row - tok * sh.group;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  if (db == 0 && g == 0) lse[(size_t)head * sh.total_q + cs.qs + tok] = l == 0.f ? -INFINITY : (m + __log2f(l)) * kCLn2;
+  __bf16* dst = out + ((size_t)(cs.qs + tok) * sh.n_heads + head) * D + db * 32 + 4 * g;
+#pragma unroll
+  for (int q4 = 0; q4 < 4; ++q4)
+    *reinterpret_cast<bf16x4*>(dst + 8 * q4) = to_bf16x4(f32x4{o[4 * q4], o[4 * q4 + 1], o[4 * q4 + 2], o[4 * q4 + 3]} * inv);
+}
+
+// Rows of a workgroup's tile.  256 where keys are many, for half the K/V traffic per product, if the chip is full of such
+// tiles or of long pieces of them; else 128, whose units take half as long.  No more than the longest sequence has, down to 32 (a
+// token or two against many keys: a wavefront without rows only takes LDS).  Measured at head_dim 128, 256 and 128 rows: 2,000 tokens x
+// 16/4 heads 50 and 37 us, 4,000 98 and 83, 6,000 x 32/8 284 with 256; in pieces 512 + 130 queries x 18,432 + 7,001 keys x 32/8
+// 179 and 225, 8,000 tokens x 2/1 69 and 89, 64 queries x 30,000 keys x 32/8 57 and 52.
+static int causal_rows(const XSegTable& segs, const CausalShape& sh, int head_dim) {
+  int longest = 0;
+  long long rows = 0, tiles = 0, units = 0;
+  for (int s = 0; s < segs.n; ++s) {
+    const long long r = (long long)segs.ql[s] * sh.group, n = (r + 255) / 256;
+    longest = longest > segs.kl[s] ? longest : segs.kl[s];
+    rows = rows > r ? rows : r;
+    tiles += n;
+    units += n * (segs.kl[s] - segs.ql[s] / 2) / kCU;
+  }
+  if (rows <= 64) return rows <= 32 ? 32 : 64;
+  const int cus = compute_unit_count();
+  if (head_dim == 64 || longest <= 1024) return 128;
+  const long long share = units * sh.n_kv_heads / cus;   // units per CU, were they dealt evenly; split if the longest tile has many more
+  return tiles * sh.n_kv_heads >= cus || (share >= 30 && longest / kCU * 2 >= 5 * share) ? 256 : 128;
+}
+// Workgroups that a split call is cut for
+static int causal_slots(int rows) { return compute_unit_count() * (rows <= 64 ? 2 : 1); }
+
+size_t cattn_fwd_workspace(const XSegTable& segs, const CausalShape& sh, int head_dim) {
+  SplitPlan plan;
+  const int rows = causal_rows(segs, sh, head_dim);
+  if (!make_split(segs, sh, rows, head_dim, causal_slots(rows), &plan)) return 0;
+  return (size_t)2 * plan.pieces * sh.n_kv_heads * (rows / 32) * (32 * head_dim + 64) * sizeof(float);
+}
+
+template <int D, int W>
+static hipError_t launch_cfg(const __bf16* q, const __bf16* k, const __bf16* v, const XSegTable& segs, const CausalShape& sh,
+                             __bf16* out, float* lse, float* workspace, hipStream_t stream) {
   using Cfg = CFwdCfg<D, W>;
+  SplitPlan plan;
+  if (make_split(segs, sh, Cfg::kRows, D, causal_slots(Cfg::kRows), &plan)) {
+    auto kern = cattn_fwd_split_kernel<D, W>;
+    hipError_t e = allow_lds(kern, Cfg::kLdsBytes);
+    if (e != hipSuccess) return e;
+    e = launch(kern, dim3(plan.pieces * sh.n_kv_heads), dim3(W * 64), Cfg::kLdsBytes, stream, q, k, v, out, lse, plan, sh, workspace);
+    if (e != hipSuccess) return e;
+    return launch(cattn_fwd_join_kernel<D, W>, dim3((plan.pieces - 1) * sh.n_kv_heads, W), dim3(D * 2 * kJoinShares), 0, stream, out, lse, plan, sh,
+                  (const float*)workspace);
+  }
   const TileIndex ti = make_causal_index<false>(segs, sh.group, Cfg::kRows);
   const int tiles = count_tiles(ti);
   if (tiles == 0) return hipSuccess;
   auto kern = cattn_fwd_kernel<D, W>;
   hipError_t e = allow_lds(kern, Cfg::kLdsBytes);
   if (e != hipSuccess) return e;
-  return launch(kern, dim3((unsigned)tiles * sh.n_kv_heads), dim3(W * 64), Cfg::kLdsBytes, stream, (const __bf16*)q,
-                (const __bf16*)k, (const __bf16*)v, (__bf16*)out, lse, segs, ti, sh);
+  return launch(kern, dim3((unsigned)tiles * sh.n_kv_heads), dim3(W * 64), Cfg::kLdsBytes, stream, q, k, v, out, lse, segs, ti, sh);
 }
 
 hipError_t launch_cattn_fwd(const void* q, const void* k, const void* v, const XSegTable& segs, const CausalShape& sh,
-                            int head_dim, void* out, float* lse, hipStream_t stream) {
-  if (head_dim == 64) return launch_cfg<64, 4>(q, k, v, segs, sh, out, lse, stream);
-  int longest = 0;
-  for (int s = 0; s < segs.n; ++s) longest = longest > segs.kl[s] ? longest : segs.kl[s];
-  if (longest <= 1024) return launch_cfg<128, 4>(q, k, v, segs, sh, out, lse, stream);
-  return launch_cfg<128, 8>(q, k, v, segs, sh, out, lse, stream);
+                            int head_dim, void* out, float* lse, void* workspace, hipStream_t stream) {
+  const int rows = causal_rows(segs, sh, head_dim);
+  auto run = head_dim == 64 ? (rows == 32 ? launch_cfg<64, 1> : rows == 64 ? launch_cfg<64, 2> : launch_cfg<64, 4>)
+             : rows == 32   ? launch_cfg<128, 1>
+             : rows == 64   ? launch_cfg<128, 2>
+             : rows == 128  ? launch_cfg<128, 4>
+                            : launch_cfg<128, 8>;
+  return run((const __bf16*)q, (const __bf16*)k, (const __bf16*)v, segs, sh, (__bf16*)out, lse, (float*)workspace, stream);
 }
 
 }  // namespace vfm

@@ -82,6 +82,17 @@ bool good_scale(float scale) { return scale > 0.f && isfinite(scale) && isfinite
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
+// Workspace of a causal forward: the runs follow one another on the stream and share it.
+size_t fwd_workspace(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, const CausalShape& sh, int head_dim) {
+  size_t most = 0;
+  for (int s0 = 0; s0 < n_seqs; s0 += VFM_MAX_XSEQS) {
+    XSegTable segs;
+    build_table(cu_q + s0, cu_kv + s0, std::min(VFM_MAX_XSEQS, n_seqs - s0), &segs);
+    most = std::max(most, vfm::cattn_fwd_workspace(segs, sh, head_dim));
+  }
+  return align_up(most, 256);
+}
+
 int check_pages(int n_pages, int max_pages, int page_size) {
   if (n_pages < 0 || max_pages < 0 || page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1))) return VFM_ERR_PAGE;
   return VFM_OK;
@@ -116,8 +127,10 @@ extern "C" {
 
 size_t vfm_cattn_fwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs, int total_q,
                                     int total_kv, int n_heads, int n_kv_heads, int head_dim) {
-  (void)cu_seqlens_q; (void)cu_seqlens_kv; (void)n_seqs; (void)total_q; (void)total_kv; (void)n_heads; (void)n_kv_heads; (void)head_dim;
-  return 0;
+  if (!cu_seqlens_q || !cu_seqlens_kv ||
+      check_causal(cu_seqlens_q, cu_seqlens_kv, n_seqs, total_q, total_kv, n_heads, n_kv_heads, head_dim))
+    return 0;
+  return fwd_workspace(cu_seqlens_q, cu_seqlens_kv, n_seqs, make_shape(total_q, n_heads, n_kv_heads, 0, 0, 0, 1.f), head_dim);
 }
 
 int vfm_cattn_fwd(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -136,12 +149,13 @@ int vfm_cattn_fwd(const void* q, int64_t q_stride, const void* k, int64_t k_stri
   if (!st) st = check_span(cu_seqlens_kv, n_seqs, std::max(k_stride, v_stride));
   if (st) return st;
   if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(out, 16) || !aligned(lse, 16)) return VFM_ERR_ALIGN;
-  (void)workspace; (void)workspace_bytes;
   const CausalShape sh = make_shape(total_q, n_heads, n_kv_heads, q_stride, k_stride, v_stride, scale);
+  const size_t need = fwd_workspace(cu_seqlens_q, cu_seqlens_kv, n_seqs, sh, head_dim);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need)) return VFM_ERR_WORKSPACE;
   for (int s0 = 0; s0 < n_seqs; s0 += VFM_MAX_XSEQS) {
     XSegTable segs;
     build_table(cu_seqlens_q + s0, cu_seqlens_kv + s0, std::min(VFM_MAX_XSEQS, n_seqs - s0), &segs);
-    hipError_t e = vfm::launch_cattn_fwd(q, k, v, segs, sh, head_dim, out, lse, static_cast<hipStream_t>(hip_stream));
+    hipError_t e = vfm::launch_cattn_fwd(q, k, v, segs, sh, head_dim, out, lse, workspace, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return vfm::launch_status(e);
   }
   return VFM_OK;
