@@ -179,6 +179,23 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
 }
 
 // ---------------------------------------------------------------- launch
+// Wavefronts that share the keys of a dK/dV workgroup (RG of cattn_dkdv_kernel): 1 where the workgroups of 128 keys keep the chip
+// busy; more where the longest of them, which walks all of its sequence's rows, takes longer than an even share of the
+// work.
+static int dkdv_shares(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
+  long long longest = 0, work = 0;                 // in 64-row tiles
+  for (int s = 0; s < segs.n; ++s) {
+    const long long tiles = ((long long)segs.ql[s] * sh.group + 63) / 64, n = (segs.kl[s] + kCBwdBC - 1) / kCBwdBC;
+    // keys before the first query are seen by all rows, the others by half of them on average
+    const long long before = segs.kl[s] > segs.ql[s] ? (segs.kl[s] - segs.ql[s]) / kCBwdBC : 0;
+    longest = longest > tiles ? longest : tiles;
+    work += before * tiles + (n - before) * (tiles + 1) / 2;
+  }
+  const long long share = work * sh.n_kv_heads / cus;
+  if (longest <= share + share / 2 + 4) return 1;
+  return head_dim == 64 && longest > 3 * share ? 4 : 2;
+}
+
 template <int D>
 static hipError_t launch_bwd_dim(const __bf16* q, const __bf16* k, const __bf16* v, const __bf16* out, const float* lse,
                                  const __bf16* dout, const XSegTable& segs, const CausalShape& sh, __bf16* dq,
@@ -195,14 +212,21 @@ static hipError_t launch_bwd_dim(const __bf16* q, const __bf16* k, const __bf16*
                segs, tq, sh, dq_row);
     if (e != hipSuccess) return e;
   }
-  const TileIndex tk = make_causal_index<true>(segs, sh.group, kCBwdBC);
-  const int n = count_tiles(tk);
-  if (n == 0) return hipSuccess;
-  using Cfg = CKvCfg<D>;
-  hipError_t e = allow_lds(cattn_dkdv_kernel<D>, Cfg::kLdsBytes);
-  if (e != hipSuccess) return e;
-  return launch(cattn_dkdv_kernel<D>, dim3((unsigned)n * sh.n_kv_heads), dim3(256), Cfg::kLdsBytes, stream, q, k, v, dout, lse2,
-                delta, sentinel, dk, dv, segs, tk, sh, dk_row, dv_row);
+  auto keys_pass = [&](auto rg_c) -> hipError_t {
+    constexpr int RG = decltype(rg_c)::value;
+    using Cfg = CKvCfg<D, RG>;
+    const TileIndex tk = make_causal_index<true>(segs, sh.group, Cfg::kBC);
+    const int n = count_tiles(tk);
+    if (n == 0) return hipSuccess;
+    hipError_t e = allow_lds(cattn_dkdv_kernel<D, RG>, Cfg::kLdsBytes);
+    if (e != hipSuccess) return e;
+    return launch(cattn_dkdv_kernel<D, RG>, dim3((unsigned)n * sh.n_kv_heads), dim3(256), Cfg::kLdsBytes, stream, q, k, v, dout,
+                  lse2, delta, sentinel, dk, dv, segs, tk, sh, dk_row, dv_row);
+  };
+  const int rg = dkdv_shares(segs, sh, D, compute_unit_count());
+  if constexpr (D == 64)
+    if (rg == 4) return keys_pass(IntC<4>{});
+  return rg == 1 ? keys_pass(IntC<1>{}) : keys_pass(IntC<2>{});
 }
 
 hipError_t launch_cattn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,

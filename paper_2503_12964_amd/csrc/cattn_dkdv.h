@@ -9,6 +9,10 @@
 //    conditional correction, no division.
 //  - The walk begins at the tile of the first row that sees any of the keys, a wavefront's at the first that sees any of
 //    its own (in steps of the ring, so that every LDS address stays an immediate).
+//  - With K/V heads shared by a group there are few of them, and a call of a few sequences may be fewer workgroups than the chip has
+//    room for, the longest taking as long as its rows are many.  RG = 2 or 4: the four wavefronts own 64 or 32 keys, RG of
+//    them the same ones; each takes one 32-row block of every tile, and their sums are added in order at the end.  With one block
+//    per tile the row operands of a block are read two tiles ahead, so that the ring has a fourth stage.
 //  - Scores of pairs that are not seen become -inf before their exponentials, in the blocks that cross the diagonal only.
 #pragma once
 
@@ -17,32 +21,40 @@
 namespace vfm {
 
 constexpr int kCBwdWaves = 4;
-constexpr int kCBwdBC = 128;   // keys per workgroup
-constexpr int kCBwdBQ = 64;    // rows per LDS tile
-constexpr int kCBwdRing = 3;
+constexpr int kCBwdBC = 128;   // keys per workgroup (RG = 1)
 constexpr int kSgbValu = 0x002, kSgbMfma = 0x008, kSgbDsRead = 0x100;
 
-template <int D>
+template <int D, int RG>
 struct CKvCfg {
-  static constexpr int kTileBytes = kCBwdBQ * D * 2;                     // one Q or dO tile
+  static constexpr int kBC = kCBwdBC / RG;                               // keys per workgroup
+  static constexpr int kBQ = RG == 4 ? 128 : 64;                         // rows per LDS tile
+  static constexpr int kBlocks = kBQ / 32 / RG;                          // row blocks of a tile that a wavefront takes
+  static constexpr int kRing = RG == 1 ? 3 : 4;                          // LDS stages
+  static constexpr int kAhead = kRing - 1;                               // tiles requested ahead
+  static constexpr int kTileBytes = kBQ * D * 2;                         // one Q or dO tile
   static constexpr int kStageBytes = 2 * kTileBytes;
-  static constexpr int kStatBytes = 4 * kCBwdBQ * 4;                     // lse2, Delta (+ spare) of one stage
-  static constexpr int kStatBase = kCBwdRing * kStageBytes;
-  static constexpr int kOwnK = 2 * kStageBytes;                          // K rows on their way: the ring's last stage
-  static constexpr int kOwnV = kStatBase + kCBwdRing * kStatBytes;       // V rows: behind the statistics
-  static constexpr int kLdsBytes = kOwnV + kCBwdBC * D * 2;
-  static_assert(kCBwdBC * D * 2 <= kStageBytes && kOwnV % 1024 == 0 && kLdsBytes <= 160 * 1024, "K rows fit a stage; LDS of one CU");
+  static constexpr int kStatBytes = 4 * kBQ * 4;                         // lse2, Delta (+ spare) of one stage
+  static constexpr int kStatBase = kRing * kStageBytes;
+  // K and V rows on their way into registers: over the ring's last stage, which fills after the prologue (RG = 1: V behind the
+  // statistics; else wavefronts of the same keys share a copy)
+  static constexpr int kOwnK = (kRing - 1) * kStageBytes;
+  static constexpr int kOwnV = RG == 1 ? kStatBase + kRing * kStatBytes : kOwnK + kBC * D * 2;
+  static constexpr int kLdsBytes = RG == 1 ? kOwnV + kCBwdBC * D * 2 : kStatBase + kRing * kStatBytes;
+  static constexpr int kTurn = 4 / RG * 32 * D * 2;                      // results on their way out, then (RG > 1) the others' sums
+  static_assert(kBC * D * 2 * (RG == 1 ? 1 : 2) <= kStageBytes && kOwnV % 1024 == 0 && kLdsBytes <= 160 * 1024, "own rows fit a stage; LDS of one CU");
+  static_assert(kTurn + (RG - 1) * (4 / RG) * 2 * 32 * D * 4 <= kStatBase, "the others' sums");
   static constexpr int kChunksPerRow = D / 8;
-  static constexpr int kLoadsPerWave = kCBwdBQ * kChunksPerRow / (kCBwdWaves * 64);
+  static constexpr int kLoadsPerWave = kBQ * kChunksPerRow / (kCBwdWaves * 64);
 };
 
-template <int D>
-__global__ __launch_bounds__(kCBwdWaves * 64, D == 64 ? 2 : 1)
+template <int D, int RG>
+__global__ __launch_bounds__(kCBwdWaves * 64, D == 64 && RG < 4 ? 2 : 1)
 void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
                        const __bf16* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ delta,
                        const float* __restrict__ sentinel, __bf16* __restrict__ dk, __bf16* __restrict__ dv,
                        const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dk_row, uint32_t dv_row) {
-  using Cfg = CKvCfg<D>;
+  using Cfg = CKvCfg<D, RG>;
+  constexpr int kBQ = Cfg::kBQ;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int LPW = Cfg::kLoadsPerWave;
   constexpr int SB = Cfg::kStageBytes;
@@ -54,16 +66,17 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
 
   const int kvh = blockIdx.x % sh.n_kv_heads;
   int seq, tk;
-  locate_tile(ti, segs.n, blockIdx.x / sh.n_kv_heads, seq, tk);   // a sequence's first keys, which most rows see, first
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads, seq, tk);   // a sequence's first keys, which most rows see, first
   const CausalSeq cs = causal_seq(segs, seq, sh.group);
-  const int j0 = tk * kCBwdBC;
+  const int j0 = tk * Cfg::kBC;
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63;
   const int c = lane & 31;
   const int g = lane >> 5;
-  const int jw = j0 + wave * 32;                       // the wavefront's first key
+  const int rg = wave / (kCBwdWaves / RG);             // which of a tile's row blocks it takes (RG > 1)
+  const int jw = j0 + wave % (kCBwdWaves / RG) * 32;   // the wavefront's first key
   const int keys_valid = cs.kl - jw;
   auto kv_row0 = [&](__bf16* base, uint32_t row_bytes) {
     return reinterpret_cast<__bf16*>(reinterpret_cast<char*>(base) + (size_t)(cs.ks + jw) * row_bytes) + kvh * D;
@@ -74,10 +87,10 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     const long long r = ((long long)j - cs.off) * sh.group;
     return r < 0 ? 0 : r > 0x7fffffffLL ? 0x7fffffff : (int)r;
   };
-  const int rt0 = first_row(j0) / kCBwdBQ * kCBwdBQ;
-  const int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kCBwdBQ - 1) / kCBwdBQ : 0;
+  const int rt0 = first_row(j0) / kBQ * kBQ;
+  const int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kBQ - 1) / kBQ : 0;
   if (n_tiles == 0) {      // keys of a sequence without queries
-    if (c < keys_valid) {
+    if (rg == 0 && c < keys_valid) {
       const u32x2 z = {0u, 0u};
 #pragma unroll
       for (int x = 0; x < D / 8; ++x) {
@@ -90,15 +103,16 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   const int row_min = first_row(jw + c);               // of this lane's key
   const int wave_all = __builtin_amdgcn_readfirstlane(first_row(jw + 31));   // rows from here on see all of the wavefront's keys
   // tiles whose rows see none of the wavefront's keys, in whole turns of the ring
-  int skip = __builtin_amdgcn_readfirstlane((first_row(jw) - rt0) / kCBwdBQ);
-  skip = (skip < n_tiles ? skip : n_tiles - 1) / kCBwdRing * kCBwdRing;
+  int skip = __builtin_amdgcn_readfirstlane((first_row(jw) - rt0) / kBQ);
+  skip = (skip < n_tiles ? skip : n_tiles - 1) / Cfg::kRing * Cfg::kRing;
 
   // ---- tile requests (direct global->LDS).  Lane L of wave instruction (x, wave) owns LDS chunk (x*waves + wave)*64 + L:
   // row P / chunks_per_row, physical chunk P % chunks_per_row (the swizzle has a period of 16 rows, so the logical chunk
   // does not depend on x).  Offsets count from the sequence's first query and step by 64 rows; past the last row
-  // they clamp to it.  Waves 0/2 fetch lse2, waves 1/3 Delta of the 64 rows (2 and 3 into spare LDS).
+  // they clamp to it.  Waves 0/2 fetch lse2, waves 1/3 Delta: 0 and 1 of a tile's first 64 rows, 2 and 3 of the others (of the
+  // same into spare LDS where there are none).
   const uint32_t do_row = (uint32_t)sh.n_heads * RB;
-  const int d_tok = kCBwdBQ / sh.group, d_sub = kCBwdBQ - d_tok * sh.group;
+  const int d_tok = kBQ / sh.group, d_sub = kBQ - d_tok * sh.group;
   const uint32_t q_step = (uint32_t)d_tok * sh.q_row + (uint32_t)d_sub * RB, q_wrap = sh.q_row - (uint32_t)sh.group * RB;
   const uint32_t do_step = (uint32_t)d_tok * do_row + (uint32_t)d_sub * RB, do_wrap = do_row - (uint32_t)sh.group * RB;
   const uint32_t q_last = (uint32_t)(cs.ql - 1) * sh.q_row + (uint32_t)(sh.group - 1) * RB;
@@ -118,14 +132,16 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     do_off[x] = (uint32_t)tok * do_row + (uint32_t)sub[x] * RB;
   }
   const bool is_lse = (wave & 1) == 0;
+  const int stat_half = kBQ == 128 ? wave >> 1 : 0;
   const float* stat_src = uniform_ptr(is_lse ? lse2 : delta);
   const uint32_t stat_sentinel = (uint32_t)((const char*)(sentinel + (is_lse ? 0 : 1)) - (const char*)stat_src);
-  int stat_row = rt0 + lane, stat_sub = stat_row % sh.group;
+  int stat_row = rt0 + 64 * stat_half + lane, stat_sub = stat_row % sh.group;
   uint32_t stat_off = ((uint32_t)(kvh * sh.group + stat_sub) * sh.total_q + cs.qs + stat_row / sh.group) * 4u;
   const uint32_t stat_step = ((uint32_t)d_sub * sh.total_q + d_tok) * 4u, stat_wrap = 4u - (uint32_t)sh.group * sh.total_q * 4u;
   const uint32_t smem_addr = lds_addr_of(smem);
   const uint32_t wave_lds = __builtin_amdgcn_readfirstlane(smem_addr + wave * 1024);
-  const uint32_t stat_lds = __builtin_amdgcn_readfirstlane(smem_addr + Cfg::kStatBase + wave * (kCBwdBQ * 4));
+  const uint32_t stat_lds = __builtin_amdgcn_readfirstlane(
+      smem_addr + Cfg::kStatBase + (kBQ == 128 ? (wave & 1) * 128 + stat_half * 64 : wave * 64) * 4);
   auto issue_tile = [&](int stage) {
 #pragma unroll
     for (int x = 0; x < LPW; ++x) {
@@ -139,7 +155,7 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
       sub[x] -= wrap ? sh.group : 0;
     }
     lds_dma4(stat_src, stat_row < cs.rows ? stat_off : stat_sentinel, stat_lds + stage * Cfg::kStatBytes);
-    stat_row += kCBwdBQ;
+    stat_row += kBQ;
     stat_sub += d_sub;
     const bool wrap = stat_sub >= sh.group;
     stat_off += stat_step + (wrap ? stat_wrap : 0u);
@@ -152,20 +168,20 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
 #pragma unroll
   for (int t = 0; t < 2; ++t)
     tbase[t] = tile_off<D>(8 * t + 4 * g + ((lane & 15) >> 2), 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
-  constexpr int SETS = kCBwdRing * SB > 65536 ? 2 : 1;   // set 1: stage 2, beyond the 64 KB an immediate reaches
+  constexpr int SETS = Cfg::kRing * SB > 65536 ? 2 : 1;   // set 1: stages 2 and 3, beyond the 64 KB an immediate reaches
   uint32_t rb[SETS][KS], tb[SETS][2][DB];
 #pragma unroll
   for (int hs = 0; hs < SETS; ++hs) {
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      rb[hs][ks] = smem_addr + hs * 2 * SB + (rbase ^ (ks << 5));
+      rb[hs][ks] = smem_addr + hs * 2 * SB + (rbase ^ (ks << 5)) + rg * 32 * RB;
       asm volatile("" : "+v"(rb[hs][ks]));
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        tb[hs][t][db] = smem_addr + hs * 2 * SB + (tbase[t] ^ (db << 6));
+        tb[hs][t][db] = smem_addr + hs * 2 * SB + (tbase[t] ^ (db << 6)) + rg * 32 * RB;
         asm volatile("" : "+v"(tb[hs][t][db]));
       }
   }
@@ -185,7 +201,7 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   };
 
   // ---- prologue: K, V rows, tiles 0 and 1 requested
-  const uint32_t own = smem_addr + wave * (32 * RB);   // this wavefront's rows, from kOwnK and kOwnV on
+  const uint32_t own = smem_addr + wave % (kCBwdWaves / RG) * (32 * RB);   // this wavefront's rows, from kOwnK and kOwnV on
   {
     const char* kbase = uniform_ptr((const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB);
     const char* vbase = uniform_ptr((const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB);
@@ -198,7 +214,8 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
       lds_dma16(vbase, key * sh.v_row + col, own_s + Cfg::kOwnV + x * 1024);
     }
   }
-  issue_tile(0); issue_tile(1);
+#pragma unroll
+  for (int t = 0; t < Cfg::kAhead; ++t) issue_tile(t);
   wait_vmcnt<0>();
   bf16x8 kreg[KS], vreg[KS];
 #pragma unroll
@@ -213,18 +230,19 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   // tiles that the wavefront does not compute (none of its keys exist, or none is seen yet): its share of the requests, the
   // waits and barriers
   const int idle_tiles = keys_valid <= 0 ? n_tiles : skip;
-  for (int t = 0; t < idle_tiles; t += kCBwdRing) {
+  for (int t = 0; t < idle_tiles; t += Cfg::kRing) {
 #pragma unroll
-    for (int x = 0; x < kCBwdRing; ++x)
+    for (int x = 0; x < Cfg::kRing; ++x)
       if (t + x < idle_tiles) {
         wait_vmcnt<0>();
         __syncthreads();
-        issue_tile((x + 2) % kCBwdRing);
+        issue_tile((x + Cfg::kAhead) % Cfg::kRing);
       }
   }
   if (keys_valid <= 0) {
     wait_vmcnt<0>();
     __syncthreads();
+    if constexpr (RG > 1) __syncthreads();
     return;
   }
 
@@ -233,7 +251,7 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   {
     bf16x8 q0r[KS], d0r[KS];
     read_rows(0, 0, q0r, d0r);
-    read_rows(0, 1, qa_n, da_n);
+    if constexpr (Cfg::kBlocks == 2) read_rows(0, 1, qa_n, da_n); else read_rows(1, 0, qa_n, da_n);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       if constexpr (kAsm) {
@@ -247,26 +265,28 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     if constexpr (kAsm) wait_mfma_v(s_cur, dp_cur);
   }
 
-  // One pipeline iteration; POS = b % 6 fixes every LDS stage at compile time.  row0: first row of block b.
+  // One pipeline iteration; POS = b % (3 blocks of a tile) fixes every LDS stage at compile time.  row0: first row of block b.
   auto iteration = [&](auto pos_c, int row0) {
     constexpr int POS = decltype(pos_c)::value;
-    constexpr int IB = POS & 1;                           // block b within its tile
-    constexpr int ST_CUR = (POS / 2) % kCBwdRing;         // stage of block b's tile
-    constexpr int ST_ROW = ((POS + 2) / 2) % kCBwdRing;   // stage of block b+2's tile
+    constexpr int NB = Cfg::kBlocks;
+    constexpr int IB = POS % NB;                            // block b within its tile
+    constexpr int ST_CUR = (POS / NB) % Cfg::kRing;          // stage of block b's tile
+    constexpr int ST_ROW = ((POS + 2) / NB) % Cfg::kRing;    // stage of block b+2's tile
+    constexpr int IB_ROW = (POS + 2) % NB;
     if constexpr (IB == 0) {
-      // Start of tile t = b/2: tile t+1 must have landed for every wave before anyone reads
-      // block b+2's rows, and every wave is past tile t-1, whose stage takes tile t+2.
+      // Start of tile t: what was requested has landed for every wave before anyone reads block b+2's rows (tile t+1;
+      // one block per tile: t+2), and every wave is past tile t-1, whose stage takes the next.
       wait_vmcnt<0>();
       __syncthreads();
-      issue_tile((ST_CUR + 2) % kCBwdRing);
+      issue_tile((ST_CUR + Cfg::kAhead) % Cfg::kRing);
     }
     if (row0 < wave_all) {   // (wave-uniform) the block crosses the diagonal: rows that do not see this lane's key
 #pragma unroll
       for (int e = 0; e < 16; ++e)
         if (row0 + 8 * (e >> 2) + 4 * g + (e & 3) < row_min) s_cur[e] = -INFINITY;
     }
-    const float* lse_s = reinterpret_cast<const float*>(smem + Cfg::kStatBase + ST_CUR * Cfg::kStatBytes);
-    const float* delta_s = lse_s + kCBwdBQ;              // wave 1's statistics follow wave 0's
+    const float* lse_s = reinterpret_cast<const float*>(smem + Cfg::kStatBase + ST_CUR * Cfg::kStatBytes) + rg * 32;
+    const float* delta_s = lse_s + kBQ;
 
     // ---- phase A: S(b+1), dP(b+1) | P(b) | statistics and transposed-operand reads of block b (one group per product)
     constexpr int NG = 2 * KS;
@@ -355,7 +375,7 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
       for (int db = 0; db < DB; ++db)
         dkacc[db] = mfma32(join_tr(qlo[s2][db], qhi[s2][db]), dsb[s2], dkacc[db]);
     bf16x8 qa_2[KS], da_2[KS];
-    read_rows(ST_ROW, IB, qa_2, da_2);
+    read_rows(ST_ROW, IB_ROW, qa_2, da_2);
 #pragma unroll
     for (int i = 0; i < 2 * DB; ++i) {
       __builtin_amdgcn_sched_group_barrier(kSgbMfma, 1, 0);
@@ -369,18 +389,52 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     for (int ks = 0; ks < KS; ++ks) { qa_n[ks] = qa_2[ks]; da_n[ks] = da_2[ks]; }
   };
 
-  static_assert(kCBwdRing == 3, "the block loop is unrolled over the ring");
-  for (int t = skip; t < n_tiles; t += 3) {
-    const int row = rt0 + t * kCBwdBQ;
-    iteration(IntC<0>{}, row);
-    iteration(IntC<1>{}, row + 32);
-    if (t + 1 < n_tiles) { iteration(IntC<2>{}, row + 64); iteration(IntC<3>{}, row + 96); }
-    if (t + 2 < n_tiles) { iteration(IntC<4>{}, row + 128); iteration(IntC<5>{}, row + 160); }
+  for (int t = skip; t < n_tiles; t += Cfg::kRing) {
+    const int row = rt0 + t * kBQ;
+    if constexpr (RG == 1) {
+      iteration(IntC<0>{}, row);
+      iteration(IntC<1>{}, row + 32);
+      if (t + 1 < n_tiles) { iteration(IntC<2>{}, row + 64); iteration(IntC<3>{}, row + 96); }
+      if (t + 2 < n_tiles) { iteration(IntC<4>{}, row + 128); iteration(IntC<5>{}, row + 160); }
+    } else {
+      iteration(IntC<0>{}, row + rg * 32);
+      if (t + 1 < n_tiles) iteration(IntC<1>{}, row + kBQ + rg * 32);
+      if (t + 2 < n_tiles) iteration(IntC<2>{}, row + 2 * kBQ + rg * 32);
+      if (t + 3 < n_tiles) iteration(IntC<3>{}, row + 3 * kBQ + rg * 32);
+    }
   }
   wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
 
   // ---- epilogue: dK (scaled) and dV of this wavefront's keys
   __syncthreads();   // the ring is free: each wavefront turns its tiles through a piece of it
+  if constexpr (RG > 1) {
+    const int ln = lane_anew(), kb = wave % (kCBwdWaves / RG);
+    auto sums = [&](int r) { return reinterpret_cast<f32x4*>(smem + Cfg::kTurn) + (size_t)((r - 1) * (kCBwdWaves / RG) + kb) * (2 * 8 * D); };
+    if (rg > 0) {
+      f32x4* to = sums(rg);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          to[(db * 4 + q4) * 64 + ln] = f32x4{dkacc[db][4 * q4], dkacc[db][4 * q4 + 1], dkacc[db][4 * q4 + 2], dkacc[db][4 * q4 + 3]};
+          to[((DB + db) * 4 + q4) * 64 + ln] = f32x4{dvacc[db][4 * q4], dvacc[db][4 * q4 + 1], dvacc[db][4 * q4 + 2], dvacc[db][4 * q4 + 3]};
+        }
+    }
+    __syncthreads();
+    if (rg > 0) return;
+#pragma unroll
+    for (int r = 1; r < RG; ++r) {
+      const f32x4* from = sums(r);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 a = from[(db * 4 + q4) * 64 + ln], b = from[((DB + db) * 4 + q4) * 64 + ln];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { dkacc[db][4 * q4 + e] += a[e]; dvacc[db][4 * q4 + e] += b[e]; }
+        }
+    }
+  }
   char* turn = smem + wave * (32 * RB);
   store_tile_rows<D>(turn, dkacc, sh.scale, kv_row0(dk, dk_row), dk_row / 2, keys_valid);
   store_tile_rows<D>(turn, dvacc, 1.0f, kv_row0(dv, dv_row), dv_row / 2, keys_valid);
