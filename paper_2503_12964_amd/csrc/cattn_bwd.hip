@@ -16,32 +16,42 @@
 
 namespace vfm {
 
-// ---------------------------------------------------------------- dQ at head_dim 64
-// 128 rows per workgroup, 32 per wavefront, three workgroups per CU: with the exponentials weighing twice as much against the products
-// as at head_dim 128, wavefronts of other workgroups fill the gaps.  Delta and the statistics as in cattn_dq2_kernel.
-template <int D>
+// ---------------------------------------------------------------- dQ, 32 rows per wavefront
+// At head_dim 64 three workgroups of four wavefronts share a CU: with the exponentials weighing twice as much against the products
+// as at head_dim 128, wavefronts of other workgroups fill the gaps.  KG = 2 or 4, at either head_dim: KG of the
+// wavefronts own the same 32 rows and take a 32-key block each of every tile; their sums are added in order at the end.
+// For calls of few sequences, where the longest row tile outlasts an even share of the work (as RG in cattn_dkdv.h).  Delta and
+// the statistics as in cattn_dq2_kernel.
+template <int D, int KG>
 struct CDqCfg {
-  static constexpr int kBR = 128;                             // rows per workgroup
-  static constexpr int kBC = 64;                              // keys per LDS tile
+  static constexpr int kBR = 128 / KG;                        // rows per workgroup
+  static constexpr int kBC = KG == 4 ? 128 : 64;              // keys per LDS tile
+  static constexpr int kBlocks = kBC / 32 / KG;               // key blocks of a tile that a wavefront takes
   static constexpr int kTileBytes = kBC * D * 2;              // K or V rows of one tile
-  static constexpr int kLdsBytes = 4 * kTileBytes;
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kRing = kStageBytes <= 32 * 1024 ? 3 : 2;
+  static constexpr int kLdsBytes = kRing * kStageBytes;
+  static constexpr int kTurn = 4 / KG * 32 * D * 2;           // results on their way out, then (KG > 1) the others' sums
+  static_assert(kTurn + (KG - 1) * (4 / KG) * 32 * D * 4 <= kLdsBytes, "the others' sums");
   static constexpr int kChunksPerRow = D / 8;
   static constexpr int kLoadsPerWave = kBC * kChunksPerRow / 256;
+  static constexpr int kWaves = D == 64 ? (KG == 1 ? 3 : KG == 2 ? 2 : 1) : 1;   // per SIMD
 };
 
-template <int D>
-__global__ __launch_bounds__(256, D == 64 ? 3 : 1)
+template <int D, int KG>
+__global__ __launch_bounds__(256, (CDqCfg<D, KG>::kWaves))
 void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
                      const __bf16* __restrict__ dout, const __bf16* __restrict__ out, const float* __restrict__ lse,
-                     float* __restrict__ lse2g, float* __restrict__ delta, float* __restrict__ sentinel, __bf16* __restrict__ dq, const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dq_row) {
-  using Cfg = CDqCfg<D>;
+                     float* __restrict__ lse2g, float* __restrict__ delta, float* __restrict__ sentinel,
+                     __bf16* __restrict__ dq, const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dq_row) {
+  using Cfg = CDqCfg<D, KG>;
   constexpr int KS = D / 16, DB = D / 32, RB = D * 2;
   constexpr int LPW = Cfg::kLoadsPerWave;
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
   const int kvh = blockIdx.x % sh.n_kv_heads;
   int seq, tq;
-  locate_tile(ti, segs.n, blockIdx.x / sh.n_kv_heads, seq, tq);
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads, seq, tq);
   const CausalSeq cs = causal_seq(segs, seq, sh.group);
   tq = (cs.rows + Cfg::kBR - 1) / Cfg::kBR - 1 - tq;           // a sequence's last rows, which see most, first
   const int r0 = tq * Cfg::kBR;
@@ -55,7 +65,8 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
     sentinel[0] = INFINITY;
     sentinel[1] = 0.f;
   }
-  const int row_w = r0 + wave * 32;
+  const int kg = wave / (4 / KG), rw = wave % (4 / KG);         // which of a tile's key blocks it takes; which rows
+  const int row_w = r0 + rw * 32;
   const int rows_valid = cs.rows - row_w;
   const int row = min(row_w + c, cs.rows - 1), tok = row / sh.group, head = kvh * sh.group + row - tok * sh.group;
   const int lim = tok + cs.off;
@@ -64,7 +75,7 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
   const int n_tiles = n_keys > 0 ? (n_keys + Cfg::kBC - 1) / Cfg::kBC : 0;
 
   const size_t stat = (size_t)head * sh.total_q + cs.qs + tok;
-  const bool keeps = g == 0 && row_w + c < cs.rows;             // this lane leaves its row's statistics
+  const bool keeps = kg == 0 && g == 0 && row_w + c < cs.rows;             // this lane leaves its row's statistics
   if (n_tiles == 0 && keeps) { lse2g[stat] = INFINITY; delta[stat] = 0.f; }
 
   const f32x16 zero16 = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -97,7 +108,7 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
     const char* vbase = uniform_ptr((const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB);
     const uint32_t smem_addr = __builtin_amdgcn_readfirstlane(lds_addr_of(smem));
     auto issue_tile = [&](int stage, int t) {
-      const uint32_t dst = smem_addr + stage * 2 * Cfg::kTileBytes + wave * 1024;
+      const uint32_t dst = smem_addr + stage * Cfg::kStageBytes + wave * 1024;
 #pragma unroll
       for (int x = 0; x < LPW; ++x) {
         const int p = (x * 4 + wave) * 64 + lane;
@@ -115,10 +126,14 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
       tbase[t] = tile_off<D>(8 * t + 4 * g + ((lane & 15) >> 2), 16 * ((lane >> 4) & 1) + 4 * (lane & 3));
 
     issue_tile(0, 0);
+    if (Cfg::kRing == 3) issue_tile(1, 1);
+    int stage = 0;
     for (int t = 0; t < n_tiles; ++t) {
-      wait_vmcnt<0>();
+      // tile t is there for everyone (with three stages the next one may be on its way; the statistics' stores are waited
+      // out once), and everyone is done with tile t - 1, whose stage takes the next
+      if (Cfg::kRing == 3 && t > 1) wait_vmcnt<2 * LPW>(); else wait_vmcnt<0>();
       __syncthreads();
-      if (t + 1 < n_tiles) issue_tile((t + 1) & 1, t + 1);
+      issue_tile(stage == 0 ? Cfg::kRing - 1 : stage - 1, t + Cfg::kRing - 1);
       if (t == 0) {
         if (wave_min < kCFewKeys) {     // (wave-uniform)
           f32x16 s, dp;
@@ -131,10 +146,12 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
         }
         if (keeps) { lse2g[stat] = lse2; delta[stat] = dlt; }
       }
-      const char* kt = smem + (t & 1) * 2 * Cfg::kTileBytes;
+      const char* kt = smem + stage * Cfg::kStageBytes;
       const char* vt = kt + Cfg::kTileBytes;
+      stage = stage + 1 == Cfg::kRing ? 0 : stage + 1;
 #pragma unroll
-      for (int jb = 0; jb < 2; ++jb) {
+      for (int x = 0; x < Cfg::kBlocks; ++x) {
+        const int jb = KG == 1 ? x : kg;
         const int j0 = t * Cfg::kBC + jb * 32;
         f32x16 s, dp, ds;
 #pragma unroll
@@ -171,47 +188,134 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
     wait_vmcnt<0>();
     __syncthreads();
   }
-  store_tile_rows_at<D>(smem + wave * (32 * RB), dqacc, sh.scale, rows_valid, [&](int r) {
-    const int rw = row_w + r, tk = rw / sh.group;
+  if constexpr (KG > 1) {
+    auto sums = [&](int x) { return reinterpret_cast<f32x4*>(smem + Cfg::kTurn) + (size_t)((x - 1) * (4 / KG) + rw) * (8 * D); };
+    if (kg > 0) {
+      f32x4* to = sums(kg);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4)
+          to[(db * 4 + q4) * 64 + lane] = f32x4{dqacc[db][4 * q4], dqacc[db][4 * q4 + 1], dqacc[db][4 * q4 + 2], dqacc[db][4 * q4 + 3]};
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int x = 1; x < KG; ++x) {
+      const f32x4* from = sums(x);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const f32x4 a = from[(db * 4 + q4) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dqacc[db][4 * q4 + e] += a[e];
+        }
+    }
+  }
+  store_tile_rows_at<D>(smem + rw * (32 * RB), dqacc, sh.scale, rows_valid, [&](int r) {
+    const int at = row_w + r, tk = at / sh.group;
     return reinterpret_cast<__bf16*>(reinterpret_cast<char*>(dq) + (size_t)(cs.qs + tk) * dq_row) +
-           (kvh * sh.group + rw - tk * sh.group) * D;
+           (kvh * sh.group + at - tk * sh.group) * D;
   });
 }
 
 // ---------------------------------------------------------------- launch
-// Wavefronts that share the keys of a dK/dV workgroup (RG of cattn_dkdv_kernel): 1 where the workgroups of 128 keys keep the chip
-// busy; more where the longest of them, which walks all of its sequence's rows, takes longer than an even share of the
-// work.
-static int dkdv_shares(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
-  long long longest = 0, work = 0;                 // in 64-row tiles
+// How the dK/dV pass is cut.  rg: wavefronts that share the keys of a workgroup (RG of cattn_dkdv_kernel): 1 where the workgroups of
+// 128 keys keep the chip busy; more where the longest of them, which walks all of its sequence's rows, takes longer than an
+// even share of the work.  splits: workgroups that share a key tile's rows, where that leaves the longest far longer still.
+// (Whole backward with rg = 1, 2, 4: head_dim 64: 2,146 and shorter x 12/4 heads 134, 101, 86 us; 6,000 x 16/4 463, 353, 370; 6,000 x
+// 32/8 609, 540, 659.  head_dim 128, rg = 1, 2: 2,000 x 16/4 227, 174; 3,000 + 2,500 x 24/8 357, 361; 6,000 x 32/8 956, 985.
+// Uncut and cut by share: head_dim 128: 1,000 x 8/2 75, 57; 2,000 x 16/4 158, 113; 4,000 x 16/4 327, 268; 8,000 x 16/1 1,918, 839;
+// 5,000 x 7/1 568, 235; 500 in two x 16/1 78, 47; head_dim 64, rg = 4
+// uncut and rg = 2 cut: 4,000 x 8/2 138, 101; 1,500 in three x 12/4 29, 34; in twice as many pieces 4,000 x 16/4 278,
+// 8,000 x 16/1 873.)
+struct KeysPlan { int rg, splits; };
+static KeysPlan keys_plan(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
+  long long longest = 0, work = 0, tiles_k = 0;    // in 64-row tiles of 128 keys
   for (int s = 0; s < segs.n; ++s) {
     const long long tiles = ((long long)segs.ql[s] * sh.group + 63) / 64, n = (segs.kl[s] + kCBwdBC - 1) / kCBwdBC;
     // keys before the first query are seen by all rows, the others by half of them on average
     const long long before = segs.kl[s] > segs.ql[s] ? (segs.kl[s] - segs.ql[s]) / kCBwdBC : 0;
     longest = longest > tiles ? longest : tiles;
     work += before * tiles + (n - before) * (tiles + 1) / 2;
+    tiles_k += n;
   }
   const long long share = work * sh.n_kv_heads / cus;
-  if (longest <= share + share / 2 + 4) return 1;
-  return head_dim == 64 && longest > 3 * share ? 4 : 2;
+  if (longest <= (head_dim == 64 ? share : share + share / 2) + 4) return {1, 1};
+  // about an even share of the work per piece, no shorter than kLeast tiles; at most eight workgroups per CU.  rg = 4 where a walk
+  // is too short to be cut
+  constexpr int kLeast = 14;
+  if (head_dim == 64 && longest > 3 * share && longest <= 4 * kLeast) return {4, 1};
+  const int rg = 2;
+  const long long piece = share > kLeast ? share : kLeast;
+  long long splits = (longest / rg + piece * 2 / 3) / piece;
+  const long long room = 8LL * cus / (tiles_k * rg * sh.n_kv_heads + 1);
+  splits = splits < room ? splits : room;
+  return {rg, (int)(splits < 2 ? 1 : splits > 16 ? 16 : splits)};
+}
+
+size_t cattn_bwd_parts(const XSegTable& segs, const CausalShape& sh, int head_dim) {
+  const KeysPlan plan = keys_plan(segs, sh, head_dim, compute_unit_count());
+  if (plan.splits == 1) return 0;
+  const int per = kCBwdBC / plan.rg;
+  size_t blocks = 0;
+  for (int s = 0; s < segs.n; ++s) blocks += (size_t)((segs.kl[s] + per - 1) / per) * (per / 32);
+  return blocks * sh.n_kv_heads * plan.splits * 64 * head_dim * sizeof(float);
+}
+
+// Wavefronts that share the rows of a dQ workgroup (KG of cattn_dq_kernel).  A workgroup takes some us for its rows and results and
+// then its time per 64-key tile; the call takes as long as the longest of them or as all of them on the chip's CUs.  In us, as measured
+// at head_dim 128 with 256 rows (KG = 1), 64 and 32, and at 64 with 128, 64 and 32.  (Whole backward, KG = 1, 2, 4: head_dim 128:
+// 1,000 tokens x 8/2 heads 95, 84, 77; 2,000 x 16/4 174, 162, 184; 4,000 x 16/4 340, 384, 432; 256 queries x 4,096 keys x 16/4 138,
+// 101, 71; head_dim 64: 1,000 x 8/2 47, 44, 41; 4,000 x 8/2 154, 143, 168; 6,000 x 16/4 351, 359, 502.)
+static int dq_shares(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
+  struct Cost { int rows; float each, tile, busy, at_once; };   // per workgroup, per tile alone, per tile on a busy CU, on a CU at once
+  static const Cost costs[2][3] = {{{256, 6.f, 1.28f, 1.28f, 1.f}, {64, 6.7f, 0.64f, 0.64f, 1.f}, {32, 7.5f, 0.35f, 0.35f, 1.f}},
+                                   {{128, 6.f, 1.15f, 0.72f, 3.f}, {64, 6.7f, 0.6f, 0.4f, 2.f}, {32, 7.5f, 0.33f, 0.47f, 1.f}}};
+  int best = 0;
+  float least = 0.f;
+  for (int x = 0; x < 3; ++x) {
+    const Cost& c = costs[head_dim == 64][x];
+    long long longest = 0, groups = 0;
+    double work = 0.;
+    for (int s = 0; s < segs.n; ++s) {
+      const long long tiles = (segs.kl[s] + 63) / 64, n = ((long long)segs.ql[s] * sh.group + c.rows - 1) / c.rows;
+      const long long before = segs.kl[s] > segs.ql[s] ? (segs.kl[s] - segs.ql[s]) / 64 : 0;
+      if (n > 0) longest = longest > tiles ? longest : tiles;
+      groups += n;
+      work += (double)n * (before + (tiles - before + 1) / 2);
+    }
+    const float alone = c.each + longest * c.tile;
+    const float all = (float)((groups * (c.each / c.at_once) + work * c.busy) * sh.n_kv_heads / cus);
+    const float t = alone > all ? alone : all;
+    if (x == 0 || t < least) { least = t; best = x; }
+  }
+  return 1 << best;
 }
 
 template <int D>
 static hipError_t launch_bwd_dim(const __bf16* q, const __bf16* k, const __bf16* v, const __bf16* out, const float* lse,
                                  const __bf16* dout, const XSegTable& segs, const CausalShape& sh, __bf16* dq,
                                  uint32_t dq_row, __bf16* dk, uint32_t dk_row, __bf16* dv, uint32_t dv_row, float* delta,
-                                 float* lse2, float* sentinel, hipStream_t stream) {
-  constexpr int kRows = D == 128 ? CDq2Cfg<128>::kBR : CDqCfg<64>::kBR;
-  constexpr int kLds = D == 128 ? CDq2Cfg<128>::kLdsBytes : CDqCfg<64>::kLdsBytes;
-  const TileIndex tq = make_causal_index<false>(segs, sh.group, kRows);
-  if (const int n = count_tiles(tq)) {
-    auto kern = [] { if constexpr (D == 128) return cattn_dq2_kernel<128>; else return cattn_dq_kernel<64>; }();
-    hipError_t e = allow_lds(kern, kLds);
+                                 float* lse2, float* sentinel, float* parts, hipStream_t stream) {
+  auto rows_pass = [&](auto kern, int rows, int lds) -> hipError_t {
+    const TileIndex tq = make_causal_index<false>(segs, sh.group, rows);
+    const int n = count_tiles(tq);
+    if (n == 0) return hipSuccess;
+    hipError_t e = allow_lds(kern, lds);
     if (e != hipSuccess) return e;
-    e = launch(kern, dim3((unsigned)n * sh.n_kv_heads), dim3(256), kLds, stream, q, k, v, dout, out, lse, lse2, delta, sentinel, dq,
-               segs, tq, sh, dq_row);
-    if (e != hipSuccess) return e;
-  }
+    return launch(kern, dim3((unsigned)n * sh.n_kv_heads), dim3(256), lds, stream, q, k, v, dout, out, lse, lse2, delta, sentinel, dq,
+                  segs, tq, sh, dq_row);
+  };
+  const int kg = dq_shares(segs, sh, D, compute_unit_count());
+  hipError_t e;
+  if (kg == 4) e = rows_pass(cattn_dq_kernel<D, 4>, CDqCfg<D, 4>::kBR, CDqCfg<D, 4>::kLdsBytes);
+  else if (kg == 2) e = rows_pass(cattn_dq_kernel<D, 2>, CDqCfg<D, 2>::kBR, CDqCfg<D, 2>::kLdsBytes);
+  else if constexpr (D == 128) e = rows_pass(cattn_dq2_kernel<D>, CDq2Cfg<D>::kBR, CDq2Cfg<D>::kLdsBytes);
+  else e = rows_pass(cattn_dq_kernel<D, 1>, CDqCfg<D, 1>::kBR, CDqCfg<D, 1>::kLdsBytes);
+  if (e != hipSuccess) return e;
+  const KeysPlan plan = keys_plan(segs, sh, D, compute_unit_count());
   auto keys_pass = [&](auto rg_c) -> hipError_t {
     constexpr int RG = decltype(rg_c)::value;
     using Cfg = CKvCfg<D, RG>;
@@ -220,22 +324,24 @@ static hipError_t launch_bwd_dim(const __bf16* q, const __bf16* k, const __bf16*
     if (n == 0) return hipSuccess;
     hipError_t e = allow_lds(cattn_dkdv_kernel<D, RG>, Cfg::kLdsBytes);
     if (e != hipSuccess) return e;
-    return launch(cattn_dkdv_kernel<D, RG>, dim3((unsigned)n * sh.n_kv_heads), dim3(256), Cfg::kLdsBytes, stream, q, k, v, dout,
-                  lse2, delta, sentinel, dk, dv, segs, tk, sh, dk_row, dv_row);
+    e = launch(cattn_dkdv_kernel<D, RG>, dim3((unsigned)n * sh.n_kv_heads * plan.splits), dim3(256), Cfg::kLdsBytes, stream, q, k, v, dout,
+                  lse2, delta, sentinel, dk, dv, segs, tk, sh, dk_row, dv_row, plan.splits, parts);
+    if (e != hipSuccess || plan.splits == 1) return e;
+    return launch(cattn_dkdv_join_kernel<D>, dim3((unsigned)n * (Cfg::kBC / 32) * sh.n_kv_heads), dim3(128), 0, stream, dk, dv, segs, tk,
+                  sh, dk_row, dv_row, Cfg::kBC, plan.splits, (const float*)parts);
   };
-  const int rg = dkdv_shares(segs, sh, D, compute_unit_count());
   if constexpr (D == 64)
-    if (rg == 4) return keys_pass(IntC<4>{});
-  return rg == 1 ? keys_pass(IntC<1>{}) : keys_pass(IntC<2>{});
+    if (plan.rg == 4) return keys_pass(IntC<4>{});
+  return plan.rg == 1 ? keys_pass(IntC<1>{}) : keys_pass(IntC<2>{});
 }
 
 hipError_t launch_cattn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
                             const void* dout, const XSegTable& segs, const CausalShape& sh, int head_dim,
                             void* dq, uint32_t dq_row, void* dk, uint32_t dk_row, void* dv, uint32_t dv_row,
-                            float* delta, float* lse2, float* sentinel, hipStream_t stream) {
+                            float* delta, float* lse2, float* sentinel, float* parts, hipStream_t stream) {
   auto run = head_dim == 128 ? launch_bwd_dim<128> : launch_bwd_dim<64>;
   return run((const __bf16*)q, (const __bf16*)k, (const __bf16*)v, (const __bf16*)out, lse, (const __bf16*)dout, segs, sh,
-             (__bf16*)dq, dq_row, (__bf16*)dk, dk_row, (__bf16*)dv, dv_row, delta, lse2, sentinel, stream);
+             (__bf16*)dq, dq_row, (__bf16*)dk, dk_row, (__bf16*)dv, dv_row, delta, lse2, sentinel, parts, stream);
 }
 
 }  // namespace vfm

@@ -102,6 +102,7 @@ size_t cattn_fwd_workspace(const XSegTable& segs, const CausalShape& sh, int hea
 hipError_t launch_cattn_bwd(const void* q, const void* k, const void* v, const void* out, const float* lse,
                             const void* dout, const XSegTable& segs, const CausalShape& sh, int head_dim,
                             void* dq, uint32_t dq_row, void* dk, uint32_t dk_row, void* dv, uint32_t dv_row,
-                            float* delta, float* lse2, float* sentinel, hipStream_t stream);
+                            float* delta, float* lse2, float* sentinel, float* parts, hipStream_t stream);
+size_t cattn_bwd_parts(const XSegTable& segs, const CausalShape& sh, int head_dim);        // bytes of `parts` that the run needs
 
 }  // namespace vfm

@@ -5,14 +5,19 @@
 // their measurements): row blocks of 32 in a software pipeline, S/dP products of block b+1 under the exponentials of block b,
 // tiles of 64 rows in a ring of three LDS stages requested two ahead, score products as assembly at head_dim 128 with K and V in
 // AGPRs.  What the causal order and the groups add:
-//  - A tile's rows are (query, head) pairs (cattn_common.h); a lane steps the addresses of its rows by 64 rows with one
+//  - A tile's rows are (query, head) pairs (cattn_common.h); a lane steps the addresses of its rows by a tile with one
 //    conditional correction, no division.
-//  - The walk begins at the tile of the first row that sees any of the keys, a wavefront's at the first that sees any of
-//    its own (in steps of the ring, so that every LDS address stays an immediate).
+//  - The walk goes from the sequence's last rows, which see all keys, back to the first row that sees any of the workgroup's keys
+//    (a wavefront's to the first that sees any of its own).  So the workgroups of an XCD, whose keys differ, begin at the same rows
+//    and stay on them together, in their L2: walked forwards, every key tile begins at its own diagonal and all are apart
+//    (8,000 tokens x 16/1 heads, four splits, whole backward: forwards 2,000 us, backwards 1,161).
 //  - With K/V heads shared by a group there are few of them, and a call of a few sequences may be fewer workgroups than the chip has
 //    room for, the longest taking as long as its rows are many.  RG = 2 or 4: the four wavefronts own 64 or 32 keys, RG of
 //    them the same ones; each takes one 32-row block of every tile, and their sums are added in order at the end.  With one block
 //    per tile the row operands of a block are read two tiles ahead, so that the ring has a fourth stage.
+//  - Where that is not enough (one K/V head for all query heads, long sequences) the walk itself is cut: `splits` workgroups take
+//    a share each of a key tile's rows and leave their sums in fp32, as they lie, in the workspace; cattn_dkdv_join_kernel adds
+//    them in order.
 //  - Scores of pairs that are not seen become -inf before their exponentials, in the blocks that cross the diagonal only.
 #pragma once
 
@@ -52,7 +57,8 @@ __global__ __launch_bounds__(kCBwdWaves * 64, D == 64 && RG < 4 ? 2 : 1)
 void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
                        const __bf16* __restrict__ dout, const float* __restrict__ lse2, const float* __restrict__ delta,
                        const float* __restrict__ sentinel, __bf16* __restrict__ dk, __bf16* __restrict__ dv,
-                       const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dk_row, uint32_t dv_row) {
+                       const XSegTable segs, const TileIndex ti, const CausalShape sh, uint32_t dk_row, uint32_t dv_row,
+                       int splits, float* __restrict__ parts) {
   using Cfg = CKvCfg<D, RG>;
   constexpr int kBQ = Cfg::kBQ;
   constexpr int KS = D / 16, DB = D / 32;
@@ -66,7 +72,8 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
 
   const int kvh = blockIdx.x % sh.n_kv_heads;
   int seq, tk;
-  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads, seq, tk);   // a sequence's first keys, which most rows see, first
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads / splits, seq, tk);   // a sequence's first keys, which most rows see, first
+  const int split = blockIdx.x / sh.n_kv_heads % splits;
   const CausalSeq cs = causal_seq(segs, seq, sh.group);
   const int j0 = tk * Cfg::kBC;
 
@@ -87,8 +94,23 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     const long long r = ((long long)j - cs.off) * sh.group;
     return r < 0 ? 0 : r > 0x7fffffffLL ? 0x7fffffff : (int)r;
   };
-  const int rt0 = first_row(j0) / kBQ * kBQ;
-  const int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kBQ - 1) / kBQ : 0;
+  int rt0 = first_row(j0) / kBQ * kBQ;
+  int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kBQ - 1) / kBQ : 0;
+  // where this wavefront's sums go if the rows are split: 32 keys of dK, then of dV, as the accumulators lie
+  f32x4* part = nullptr;
+  if (splits > 1) {
+    const int t0 = (int)((long long)n_tiles * split / splits), t1 = (int)((long long)n_tiles * (split + 1) / splits);
+    rt0 += t0 * kBQ;
+    n_tiles = t1 - t0;
+    // blocks of 32 keys, tile by tile (a sequence's last tile may have some past its end)
+    const size_t block = (size_t)(blockIdx.x / sh.n_kv_heads / splits) * (Cfg::kBC / 32) + wave % (kCBwdWaves / RG);
+    part = reinterpret_cast<f32x4*>(parts) + ((block * sh.n_kv_heads + kvh) * splits + split) * (16 * D);
+    if (n_tiles == 0) {
+      if (rg == 0 && keys_valid > 0)
+        for (int i = lane; i < 16 * D; i += 64) part[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      return;
+    }
+  }
   if (n_tiles == 0) {      // keys of a sequence without queries
     if (rg == 0 && c < keys_valid) {
       const u32x2 z = {0u, 0u};
@@ -102,14 +124,15 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   }
   const int row_min = first_row(jw + c);               // of this lane's key
   const int wave_all = __builtin_amdgcn_readfirstlane(first_row(jw + 31));   // rows from here on see all of the wavefront's keys
-  // tiles whose rows see none of the wavefront's keys, in whole turns of the ring
-  int skip = __builtin_amdgcn_readfirstlane((first_row(jw) - rt0) / kBQ);
-  skip = (skip < n_tiles ? skip : n_tiles - 1) / Cfg::kRing * Cfg::kRing;
+  const int rt_last = rt0 + (n_tiles - 1) * kBQ;       // tile t of the walk is rows rt_last - t * kBQ ..
+  // tiles of the walk until its rows see none of the wavefront's keys; none for a wavefront without keys
+  const int first_tile = first_row(jw) <= rt0 ? 0 : (first_row(jw) - rt0) / kBQ;
+  const int wave_tiles = __builtin_amdgcn_readfirstlane(keys_valid <= 0 || first_tile >= n_tiles ? 0 : n_tiles - first_tile);
 
   // ---- tile requests (direct global->LDS).  Lane L of wave instruction (x, wave) owns LDS chunk (x*waves + wave)*64 + L:
   // row P / chunks_per_row, physical chunk P % chunks_per_row (the swizzle has a period of 16 rows, so the logical chunk
-  // does not depend on x).  Offsets count from the sequence's first query and step by 64 rows; past the last row
-  // they clamp to it.  Waves 0/2 fetch lse2, waves 1/3 Delta: 0 and 1 of a tile's first 64 rows, 2 and 3 of the others (of the
+  // does not depend on x).  Offsets count from the sequence's first query and step back by a tile; past the last row
+  // they clamp to it, and so do those that the requests ahead of the walk's end bring below row 0 (wrapped, they are large).  Waves 0/2 fetch lse2, waves 1/3 Delta: 0 and 1 of a tile's first 64 rows, 2 and 3 of the others (of the
   // same into spare LDS where there are none).
   const uint32_t do_row = (uint32_t)sh.n_heads * RB;
   const int d_tok = kBQ / sh.group, d_sub = kBQ - d_tok * sh.group;
@@ -120,22 +143,24 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   const char* qbase = uniform_ptr((const char*)q + (size_t)cs.qs * sh.q_row + (size_t)kvh * sh.group * RB);
   const char* dobase = uniform_ptr((const char*)dout + ((size_t)cs.qs * sh.n_heads + (size_t)kvh * sh.group) * RB);
   static_assert(kCBwdWaves * 64 / Cfg::kChunksPerRow % 16 == 0, "rows of consecutive x: whole periods of the swizzle apart");
-  uint32_t q_off[LPW], do_off[LPW];
-  int sub[LPW];
+  constexpr int kRowsX = kCBwdWaves * 64 / Cfg::kChunksPerRow;     // rows from one x to the next
+  const int x_tok = kRowsX / sh.group, x_sub = kRowsX - x_tok * sh.group;
+  const uint32_t qx_step = (uint32_t)x_tok * sh.q_row + (uint32_t)x_sub * RB, dox_step = (uint32_t)x_tok * do_row + (uint32_t)x_sub * RB;
   const int own_row = (wave * 64 + lane) / Cfg::kChunksPerRow;
   const uint32_t colb = (uint32_t)(((lane % Cfg::kChunksPerRow) ^ swz<D>(own_row)) * 16);
-#pragma unroll
-  for (int x = 0; x < LPW; ++x) {
-    const int row = rt0 + x * (kCBwdWaves * 64 / Cfg::kChunksPerRow) + own_row, tok = row / sh.group;
-    sub[x] = row - tok * sh.group;
-    q_off[x] = (uint32_t)tok * sh.q_row + (uint32_t)sub[x] * RB;
-    do_off[x] = (uint32_t)tok * do_row + (uint32_t)sub[x] * RB;
+  int sub;                              // of the lane's row at x = 0
+  uint32_t q_off, do_off;
+  {
+    const int row = rt_last + own_row, tok = row / sh.group;
+    sub = row - tok * sh.group;
+    q_off = (uint32_t)tok * sh.q_row + (uint32_t)sub * RB;
+    do_off = (uint32_t)tok * do_row + (uint32_t)sub * RB;
   }
   const bool is_lse = (wave & 1) == 0;
   const int stat_half = kBQ == 128 ? wave >> 1 : 0;
   const float* stat_src = uniform_ptr(is_lse ? lse2 : delta);
   const uint32_t stat_sentinel = (uint32_t)((const char*)(sentinel + (is_lse ? 0 : 1)) - (const char*)stat_src);
-  int stat_row = rt0 + 64 * stat_half + lane, stat_sub = stat_row % sh.group;
+  int stat_row = rt_last + 64 * stat_half + lane, stat_sub = stat_row % sh.group;
   uint32_t stat_off = ((uint32_t)(kvh * sh.group + stat_sub) * sh.total_q + cs.qs + stat_row / sh.group) * 4u;
   const uint32_t stat_step = ((uint32_t)d_sub * sh.total_q + d_tok) * 4u, stat_wrap = 4u - (uint32_t)sh.group * sh.total_q * 4u;
   const uint32_t smem_addr = lds_addr_of(smem);
@@ -143,23 +168,30 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   const uint32_t stat_lds = __builtin_amdgcn_readfirstlane(
       smem_addr + Cfg::kStatBase + (kBQ == 128 ? (wave & 1) * 128 + stat_half * 64 : wave * 64) * 4);
   auto issue_tile = [&](int stage) {
+    uint32_t qo = q_off, dd = do_off;
+    int sb = sub;
 #pragma unroll
     for (int x = 0; x < LPW; ++x) {
       const uint32_t dst = wave_lds + stage * SB + x * kCBwdWaves * 1024;
-      lds_dma16(qbase, min(q_off[x], q_last) + colb, dst);
-      lds_dma16(dobase, min(do_off[x], do_last) + colb, dst + TB);
-      sub[x] += d_sub;
-      const bool wrap = sub[x] >= sh.group;
-      q_off[x] += q_step + (wrap ? q_wrap : 0u);
-      do_off[x] += do_step + (wrap ? do_wrap : 0u);
-      sub[x] -= wrap ? sh.group : 0;
+      lds_dma16(qbase, min(qo, q_last) + colb, dst);
+      lds_dma16(dobase, min(dd, do_last) + colb, dst + TB);
+      sb += x_sub;
+      const bool wrap = sb >= sh.group;
+      qo += qx_step + (wrap ? q_wrap : 0u);
+      dd += dox_step + (wrap ? do_wrap : 0u);
+      sb -= wrap ? sh.group : 0;
     }
-    lds_dma4(stat_src, stat_row < cs.rows ? stat_off : stat_sentinel, stat_lds + stage * Cfg::kStatBytes);
-    stat_row += kBQ;
-    stat_sub += d_sub;
-    const bool wrap = stat_sub >= sh.group;
-    stat_off += stat_step + (wrap ? stat_wrap : 0u);
-    stat_sub -= wrap ? sh.group : 0;
+    sub -= d_sub;
+    const bool back = sub < 0;
+    q_off -= q_step + (back ? q_wrap : 0u);
+    do_off -= do_step + (back ? do_wrap : 0u);
+    sub += back ? sh.group : 0;
+    lds_dma4(stat_src, (uint32_t)stat_row < (uint32_t)cs.rows ? stat_off : stat_sentinel, stat_lds + stage * Cfg::kStatBytes);
+    stat_row -= kBQ;
+    stat_sub -= d_sub;
+    const bool wrap = stat_sub < 0;
+    stat_off -= stat_step + (wrap ? stat_wrap : 0u);
+    stat_sub += wrap ? sh.group : 0;
   };
 
   // ---- per-lane LDS addresses within a tile (as in bwd_dkdv_unit): rows as A operand, transposing reads of the same rows
@@ -227,21 +259,19 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   }
   __syncthreads();
 
-  // tiles that the wavefront does not compute (none of its keys exist, or none is seen yet): its share of the requests, the
-  // waits and barriers
-  const int idle_tiles = keys_valid <= 0 ? n_tiles : skip;
-  for (int t = 0; t < idle_tiles; t += Cfg::kRing) {
-#pragma unroll
-    for (int x = 0; x < Cfg::kRing; ++x)
-      if (t + x < idle_tiles) {
-        wait_vmcnt<0>();
-        __syncthreads();
-        issue_tile((x + Cfg::kAhead) % Cfg::kRing);
-      }
-  }
+  // tiles that the wavefront does not compute: its share of the requests, the waits and barriers
+  auto idle_from = [&](int t) {
+    for (; t < n_tiles; ++t) {
+      wait_vmcnt<0>();
+      __syncthreads();
+      issue_tile((t + Cfg::kAhead) % Cfg::kRing);
+    }
+    wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
+    __syncthreads();   // the ring is free
+  };
+  // With no tile of its own a wavefront with keys still writes zeros (sums of a split walk, or none of its keys are seen here)
   if (keys_valid <= 0) {
-    wait_vmcnt<0>();
-    __syncthreads();
+    idle_from(0);
     if constexpr (RG > 1) __syncthreads();
     return;
   }
@@ -389,24 +419,23 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     for (int ks = 0; ks < KS; ++ks) { qa_n[ks] = qa_2[ks]; da_n[ks] = da_2[ks]; }
   };
 
-  for (int t = skip; t < n_tiles; t += Cfg::kRing) {
-    const int row = rt0 + t * kBQ;
+  for (int t = 0; t < wave_tiles; t += Cfg::kRing) {
+    const int row = rt_last - t * kBQ;
     if constexpr (RG == 1) {
       iteration(IntC<0>{}, row);
       iteration(IntC<1>{}, row + 32);
-      if (t + 1 < n_tiles) { iteration(IntC<2>{}, row + 64); iteration(IntC<3>{}, row + 96); }
-      if (t + 2 < n_tiles) { iteration(IntC<4>{}, row + 128); iteration(IntC<5>{}, row + 160); }
+      if (t + 1 < wave_tiles) { iteration(IntC<2>{}, row - 64); iteration(IntC<3>{}, row - 32); }
+      if (t + 2 < wave_tiles) { iteration(IntC<4>{}, row - 128); iteration(IntC<5>{}, row - 96); }
     } else {
       iteration(IntC<0>{}, row + rg * 32);
-      if (t + 1 < n_tiles) iteration(IntC<1>{}, row + kBQ + rg * 32);
-      if (t + 2 < n_tiles) iteration(IntC<2>{}, row + 2 * kBQ + rg * 32);
-      if (t + 3 < n_tiles) iteration(IntC<3>{}, row + 3 * kBQ + rg * 32);
+      if (t + 1 < wave_tiles) iteration(IntC<1>{}, row - kBQ + rg * 32);
+      if (t + 2 < wave_tiles) iteration(IntC<2>{}, row - 2 * kBQ + rg * 32);
+      if (t + 3 < wave_tiles) iteration(IntC<3>{}, row - 3 * kBQ + rg * 32);
     }
   }
-  wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
+  idle_from(wave_tiles);
 
-  // ---- epilogue: dK (scaled) and dV of this wavefront's keys
-  __syncthreads();   // the ring is free: each wavefront turns its tiles through a piece of it
+  // ---- epilogue: dK (scaled) and dV of this wavefront's keys; each wavefront turns its tiles through a piece of the ring
   if constexpr (RG > 1) {
     const int ln = lane_anew(), kb = wave % (kCBwdWaves / RG);
     auto sums = [&](int r) { return reinterpret_cast<f32x4*>(smem + Cfg::kTurn) + (size_t)((r - 1) * (kCBwdWaves / RG) + kb) * (2 * 8 * D); };
@@ -435,9 +464,52 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
         }
     }
   }
+  if (splits > 1) {
+    const int ln = lane_anew();
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        part[(db * 4 + q4) * 64 + ln] = f32x4{dkacc[db][4 * q4], dkacc[db][4 * q4 + 1], dkacc[db][4 * q4 + 2], dkacc[db][4 * q4 + 3]};
+        part[((DB + db) * 4 + q4) * 64 + ln] = f32x4{dvacc[db][4 * q4], dvacc[db][4 * q4 + 1], dvacc[db][4 * q4 + 2], dvacc[db][4 * q4 + 3]};
+      }
+    return;
+  }
   char* turn = smem + wave * (32 * RB);
   store_tile_rows<D>(turn, dkacc, sh.scale, kv_row0(dk, dk_row), dk_row / 2, keys_valid);
   store_tile_rows<D>(turn, dvacc, 1.0f, kv_row0(dv, dv_row), dv_row / 2, keys_valid);
+}
+
+// Adds the shares of 32 keys in order; wavefront 0 dK, wavefront 1 dV.  blockIdx.x: (32-key block as above, K/V head).
+template <int D>
+__global__ __launch_bounds__(128)
+void cattn_dkdv_join_kernel(__bf16* __restrict__ dk, __bf16* __restrict__ dv, const XSegTable segs, const TileIndex ti,
+                            const CausalShape sh, uint32_t dk_row, uint32_t dv_row, int keys_per_tile, int splits,
+                            const float* __restrict__ parts) {
+  constexpr int DB = D / 32;
+  __shared__ __attribute__((aligned(16))) char smem[2 * 32 * D * 2];
+  const int kvh = blockIdx.x % sh.n_kv_heads, block = blockIdx.x / sh.n_kv_heads, per = keys_per_tile / 32;
+  int seq, tk;
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, block / per, seq, tk);
+  const CausalSeq cs = causal_seq(segs, seq, sh.group);
+  const int j0 = tk * keys_per_tile + block % per * 32, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (j0 >= cs.kl) return;
+  const f32x4* part = reinterpret_cast<const f32x4*>(parts) + ((size_t)block * sh.n_kv_heads + kvh) * splits * (16 * D) + wave * (8 * D);
+  f32x16 acc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < splits; ++s, part += 16 * D)
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const f32x4 a = part[(db * 4 + q4) * 64 + lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[db][4 * q4 + e] += a[e];
+      }
+  const uint32_t row = wave == 0 ? dk_row : dv_row;
+  __bf16* to = reinterpret_cast<__bf16*>(reinterpret_cast<char*>(wave == 0 ? dk : dv) + (size_t)(cs.ks + j0) * row) + kvh * D;
+  store_tile_rows<D>(smem + wave * (32 * D * 2), acc, wave == 0 ? sh.scale : 1.0f, to, row / 2, cs.kl - j0);
 }
 
 }  // namespace vfm

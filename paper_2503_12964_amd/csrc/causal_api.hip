@@ -93,6 +93,18 @@ size_t fwd_workspace(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, cons
   return align_up(most, 256);
 }
 
+// Workspace of a causal backward: the statistics of all rows, and what the runs share for split dK/dV passes.
+size_t stats_bytes(int total_q, int n_heads) { return 2 * align_up((size_t)total_q * n_heads * sizeof(float), 256) + 256; }
+size_t bwd_parts(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, const CausalShape& sh, int head_dim) {
+  size_t most = 0;
+  for (int s0 = 0; s0 < n_seqs; s0 += VFM_MAX_XSEQS) {
+    XSegTable segs;
+    build_table(cu_q + s0, cu_kv + s0, std::min(VFM_MAX_XSEQS, n_seqs - s0), &segs);
+    most = std::max(most, vfm::cattn_bwd_parts(segs, sh, head_dim));
+  }
+  return align_up(most, 256);
+}
+
 int check_pages(int n_pages, int max_pages, int page_size) {
   if (n_pages < 0 || max_pages < 0 || page_size < 16 || page_size > (1 << 20) || (page_size & (page_size - 1))) return VFM_ERR_PAGE;
   return VFM_OK;
@@ -161,13 +173,14 @@ int vfm_cattn_fwd(const void* q, int64_t q_stride, const void* k, int64_t k_stri
   return VFM_OK;
 }
 
-// Delta and lse in log2 units (fp32 [n_heads, total_q] each, padded to 256 bytes), then 256 bytes of constants.
+// Delta and lse in log2 units (fp32 [n_heads, total_q] each, padded to 256 bytes), 256 bytes of constants, shares of dK and dV.
 size_t vfm_cattn_bwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs, int total_q,
                                     int total_kv, int n_heads, int n_kv_heads, int head_dim) {
   if (!cu_seqlens_q || !cu_seqlens_kv ||
       check_causal(cu_seqlens_q, cu_seqlens_kv, n_seqs, total_q, total_kv, n_heads, n_kv_heads, head_dim))
     return 0;
-  return 2 * align_up((size_t)total_q * n_heads * sizeof(float), 256) + 256;
+  return stats_bytes(total_q, n_heads) +
+         bwd_parts(cu_seqlens_q, cu_seqlens_kv, n_seqs, make_shape(total_q, n_heads, n_kv_heads, 0, 0, 0, 1.f), head_dim);
 }
 
 int vfm_cattn_bwd(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -194,17 +207,18 @@ int vfm_cattn_bwd(const void* q, int64_t q_stride, const void* k, int64_t k_stri
   if (total_q == 0 && total_kv == 0) return VFM_OK;
   const size_t need = vfm_cattn_bwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_seqs, total_q, total_kv, n_heads, n_kv_heads, head_dim);
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return VFM_ERR_WORKSPACE;
-  const size_t part = (need - 256) / 2;
+  const size_t stats = stats_bytes(total_q, n_heads), part = (stats - 256) / 2;
   float* delta = static_cast<float*>(workspace);
   float* lse2 = reinterpret_cast<float*>(static_cast<char*>(workspace) + part);
   float* sentinel = reinterpret_cast<float*>(static_cast<char*>(workspace) + 2 * part);
+  float* parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + stats);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const CausalShape sh = make_shape(total_q, n_heads, n_kv_heads, q_stride, k_stride, v_stride, scale);
   for (int s0 = 0; s0 < n_seqs; s0 += VFM_MAX_XSEQS) {
     XSegTable segs;
     build_table(cu_seqlens_q + s0, cu_seqlens_kv + s0, std::min(VFM_MAX_XSEQS, n_seqs - s0), &segs);
     hipError_t e = vfm::launch_cattn_bwd(q, k, v, out, lse, dout, segs, sh, head_dim, dq, (uint32_t)(2 * dq_stride), dk,
-                                         (uint32_t)(2 * dk_stride), dv, (uint32_t)(2 * dv_stride), delta, lse2, sentinel, stream);
+                                         (uint32_t)(2 * dk_stride), dv, (uint32_t)(2 * dv_stride), delta, lse2, sentinel, parts, stream);
     if (e != hipSuccess) return vfm::launch_status(e);
   }
   return VFM_OK;
