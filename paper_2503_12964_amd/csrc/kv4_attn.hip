@@ -9,11 +9,15 @@
 //    16x16x32 MFMAs as they come, with Q held in the same order; one conversion instruction makes two bf16 and applies the factor.
 //  - V is needed with keys along the contraction: its rows go through LDS (a wavefront's own 32 keys, no barrier) and come
 //    back by transposing reads, the key order of the score MFMA's accumulators, so that P is an operand as it stands.
-//  - The next 32 keys of a wavefront are in flight while the present ones are computed.
+//  - The next 32 keys of a wavefront are in flight while the present ones are computed; the pages of its next 32 steps sit in
+//    one register, a lane each, so that no fetch waits for a page number.
 //  - The lengths are only known on the device (a captured step serves any), so the key blocks of all (sequence, K/V head, row
 //    block) units form one line that every workgroup takes an equal piece of.  A unit that lies within one piece is
 //    finished there; the others leave (maximum, sum, unnormalised output) per piece in the workspace, joined by a second
 //    launch in the order of the pieces: no atomics, the same bits every time.
+// Measured in a captured graph, both launches: 64 sequences of 4000 keys, 32/8 heads, 55 us at head_dim 128 (279 MB, 5.1 TB/s;
+// the fetches alone, nothing computed: 54), 36 us at 64; one sequence of 100000 keys, 16/1 heads: 31 us, 9 of them the join and its
+// launch.
 #include "kv4_common.h"
 
 namespace vfm {
@@ -35,29 +39,32 @@ struct Kv4Shape {
   float scale_log2;
 };
 
-// The line of key blocks.  Every workgroup works it out for itself from the lengths: before[s] = blocks of the sequences
-// before s.
-struct Kv4Line {
-  int rb, nb;            // of the sequence: row blocks, key blocks
-  int kvh, rblk;         // the unit: K/V head, row block
-  long long at;          // first block of the unit
-};
+// The line of key blocks.  Every workgroup works it out for itself from the lengths.
 __device__ __forceinline__ int kv4_keys(const Kv4Cache& c, int len, int nq) {   // keys of a sequence
   if (len < 0 || nq == 0) return 0;
   const long long have = (long long)len + nq, room = (long long)c.max_pages << c.shift;
   const long long keys = have < room ? have : room;
   return (int)(keys < 0x7fffff00 ? keys : 0x7fffff00);
 }
+__device__ __forceinline__ int kv4_last(int len, int tok, int keys) {   // the last key that new token tok sees
+  const long long last = (long long)len + tok;                          // (a length may lie far past the table)
+  return last < keys ? (int)last : keys - 1;
+}
 __device__ __forceinline__ int kv4_row_blocks(int nq, const Kv4Shape& sh) { return (nq * sh.group + sh.rb_rows - 1) / sh.rb_rows; }
 
-// Fills before[0 .. 256] (LDS) for this run; returns the total.  All kKvThreads threads take part.
-__device__ __forceinline__ long long kv4_scan(const Kv4Table& t, const Kv4Cache& c, const Kv4Shape& sh, long long* before, long long* part) {
+// Fills before[] (blocks of the sequences before each) and lens for this run; returns the total.  All kKvThreads threads take part.
+struct Kv4Scan {
+  long long before[VFM_MAX_SEQS + 1], part[kKvWaves];
+  int lens[VFM_MAX_SEQS];
+};
+__device__ __forceinline__ long long kv4_scan(const Kv4Table& t, const Kv4Cache& c, const Kv4Shape& sh, Kv4Scan& m) {
   static_assert(kKvThreads == VFM_MAX_SEQS, "one sequence per thread");
   const int s = threadIdx.x, lane = s & 63, wave = s >> 6;
   long long mine = 0;
   if (s < t.n) {
-    const int nq = t.cu[s + 1] - t.cu[s];
-    const int keys = kv4_keys(c, c.lens[s], nq);
+    const int nq = t.cu[s + 1] - t.cu[s], len = c.lens[s];
+    const int keys = kv4_keys(c, len, nq);
+    m.lens[s] = len;
     mine = (long long)((keys + kKvBlockKeys - 1) / kKvBlockKeys) * kv4_row_blocks(nq, sh) * c.n_kv_heads;
   }
   long long sum = mine;
@@ -66,40 +73,42 @@ __device__ __forceinline__ long long kv4_scan(const Kv4Table& t, const Kv4Cache&
     const long long up = __shfl_up(sum, o);
     if (lane >= o) sum += up;
   }
-  if (lane == 63) part[wave] = sum;
+  if (lane == 63) m.part[wave] = sum;
   __syncthreads();
   long long base = 0, total = 0;
 #pragma unroll
   for (int w = 0; w < kKvWaves; ++w) {
-    if (w < wave) base += part[w];
-    total += part[w];
+    if (w < wave) base += m.part[w];
+    total += m.part[w];
   }
-  before[s] = base + sum - mine;
-  if (s == kKvThreads - 1) before[kKvThreads] = total;
+  m.before[s] = base + sum - mine;
+  if (s == kKvThreads - 1) m.before[kKvThreads] = total;
   __syncthreads();
   return total;
 }
-// Sequence of block x: the last one that begins at or before it and has blocks
+// Sequence of block x: the last one that begins at or before it (of several that begin there the last, the others are empty)
 __device__ __forceinline__ int kv4_find(const long long* before, long long x) {
-  int lo = 0, hi = VFM_MAX_SEQS;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (before[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
+  const int lane = threadIdx.x & 63;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < VFM_MAX_SEQS; i += 64) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(before[i + lane] <= x));
+  return __builtin_amdgcn_readfirstlane(n - 1);
 }
 
-// A piece's results: per slot rb_rows rows of (reference, sum), then rb_rows rows of D values.
+// The workspace: the line's before[] for the join, then slots.  A piece's results: per slot rb_rows rows of (reference, sum), then
+// rb_rows rows of D values.
+constexpr size_t kKvHead = (VFM_MAX_SEQS + 1 + 7) / 8 * 8 * sizeof(long long);
 template <int D>
 __device__ __forceinline__ size_t kv4_slot_floats(int rb_rows) { return (size_t)rb_rows * (D + 2); }
 
-// Workgroups of a CU: what the registers allow
-constexpr int kv4_per_cu(int D, int R) { return D == 128 ? (R == 1 ? 3 : R == 2 ? 2 : 1) : (R == 1 ? 4 : R == 2 ? 3 : 2); }
+// Workgroups of a CU: what the registers allow.  (At head_dim 128 and one row tile three would fit: 62 us instead of 55 at 64
+// sequences of 4000 keys, the line cut into more pieces than the fetches of two leave room for.)
+constexpr int kv4_per_cu(int D, int R) { return D == 128 ? (R <= 2 ? 2 : 1) : (R == 1 ? 4 : 2); }
 
 template <int D, int R>
 __global__ __launch_bounds__(kKvThreads, kv4_per_cu(D, R))
 void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cache c, const Kv4Shape sh,
-                     __bf16* __restrict__ out, float* __restrict__ lse, float* __restrict__ slots) {
+                     __bf16* __restrict__ out, float* __restrict__ lse, char* __restrict__ workspace) {
   constexpr int KS = D / 32;          // MFMAs of a 16-key score tile
   constexpr int DT = D / 16;          // 16-wide tiles of the head vector
   constexpr int LB = D / 8;           // bytes of codes per lane and key (a lane holds D/4 elements)
@@ -109,10 +118,16 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
   constexpr int kORow = D + 4;                       // padded row of the join, floats
   constexpr int kJoin = kKvWaves * 16 * kORow * 4;
   __shared__ __attribute__((aligned(16))) char smem[kKvWaves * kVBytes > kJoin ? kKvWaves * kVBytes : kJoin];
-  __shared__ long long before[VFM_MAX_SEQS + 1], part[kKvWaves];
+  __shared__ Kv4Scan scan;
   __shared__ float stat[2][kKvWaves][16];
+  float* const slots = reinterpret_cast<float*>(workspace + kKvHead);
+  const long long* before = scan.before;
 
-  const long long total = kv4_scan(t, c, sh, before, part);
+  const long long total = kv4_scan(t, c, sh, scan);
+  if (blockIdx.x == 0) {
+    reinterpret_cast<long long*>(workspace)[threadIdx.x] = before[threadIdx.x];
+    if (threadIdx.x == 0) reinterpret_cast<long long*>(workspace)[VFM_MAX_SEQS] = total;
+  }
   const long long per = (total + gridDim.x - 1) / gridDim.x;
   long long x = (long long)blockIdx.x * per;
   const long long x_first = x, x_end = x + per < total ? x + per : total;
@@ -125,9 +140,9 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
 
   while (x < x_end) {
     // ---- the unit that block x lies in
-    const int s = __builtin_amdgcn_readfirstlane(kv4_find(before, x));
+    const int s = kv4_find(before, x);
     const int q0 = t.cu[s], nq = t.cu[s + 1] - q0;
-    const int len = c.lens[s];
+    const int len = __builtin_amdgcn_readfirstlane(scan.lens[s]);
     const int keys = kv4_keys(c, len, nq);
     const int nb = (keys + kKvBlockKeys - 1) / kKvBlockKeys;
     const int n_rb = kv4_row_blocks(nq, sh);
@@ -148,9 +163,9 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
       const char* qp = q + (size_t)(q0 + tok) * sh.q_row + (size_t)(kvh * sh.group + row - tok * sh.group) * RB + g * (D / 2);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) qreg[rt][ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
-      lim[rt] = min(len + tok, keys - 1);
+      lim[rt] = kv4_last(len, tok, keys);
     }
-    const int lim_min = min(len + min(r0, rows - 1) / sh.group, keys - 1);   // (rows of a block: the first sees least)
+    const int lim_min = kv4_last(len, min(r0, rows - 1) / sh.group, keys);   // (rows of a block: the first sees least)
 
     f32x4 o[R][DT];
     float m_run[R], l_run[R];
@@ -162,70 +177,94 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
       for (int dt = 0; dt < DT; ++dt) o[rt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // ---- 32 keys of the cache on their way
-    struct Fetch { uint32_t k[2][LW], v[2][LW], kf[2], vf[2]; };
+    // ---- pages of 32 steps: lane l holds that of step l / 2, 16-key half l % 2 (which lies in one page), -1 where there is none
+    int pages, pages_at;
+    auto take_pages = [&](int blk) {
+      const long long j = ((long long)blk + (lane >> 1)) * kKvBlockKeys + wave * kKvStep + 16 * (lane & 1);
+      pages = j < keys ? kv4_page(c, s, j) : -1;
+      pages_at = blk;
+    };
+    // ---- 32 keys of the cache on their way.  No lane is masked out: places of the last page past the sequence's end are read like
+    // the others (and given the factor 1 below), a half without a page reads page 0 in its place.
+    struct Fetch { uint32_t k[2][LW], v[2][LW], factors, gone; };   // factors: see unpack; gone: bit h: half h has no page
     auto fetch = [&](int blk, Fetch& f) {
+      const int j0 = blk * kKvBlockKeys + wave * kKvStep, at = 2 * (blk - pages_at);
+      const int page[2] = {__builtin_amdgcn_readlane(pages, at), __builtin_amdgcn_readlane(pages, at + 1)};
+      f.gone = (page[0] < 0 ? 1u : 0u) | (page[1] < 0 ? 2u : 0u);
+      uint64_t row[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int j0 = blk * kKvBlockKeys + wave * kKvStep + 16 * h;    // (16 keys lie in one page)
-        const int page = j0 < keys ? kv4_page(c, s, j0) : -1;
-        const bool there = page >= 0 && j0 + li < keys;
-        if (there) {
-          const size_t row = kv4_row(c, page, kvh, j0) + li;
-          const uint32_t* kp = reinterpret_cast<const uint32_t*>(c.k4 + row * (D / 2) + g * LB);
-          const uint32_t* vp = reinterpret_cast<const uint32_t*>(c.v4 + row * (D / 2) + g * LB);
-          if constexpr (LW == 4) {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(kp), b = *reinterpret_cast<const u32x4*>(vp);
+        row[h] = kv4_row(c, max(page[h], 0), kvh, j0 + 16 * h);
+        const uint8_t* kp = c.k4 + row[h] * (D / 2) + (uint32_t)(li * (D / 2) + g * LB);
+        const uint8_t* vp = c.v4 + row[h] * (D / 2) + (uint32_t)(li * (D / 2) + g * LB);
+        if constexpr (LW == 4) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(kp), b = *reinterpret_cast<const u32x4*>(vp);
 #pragma unroll
-            for (int i = 0; i < LW; ++i) { f.k[h][i] = a[i]; f.v[h][i] = b[i]; }
-          } else {
-            const u32x2 a = *reinterpret_cast<const u32x2*>(kp), b = *reinterpret_cast<const u32x2*>(vp);
+          for (int i = 0; i < LW; ++i) { f.k[h][i] = a[i]; f.v[h][i] = b[i]; }
+        } else {
+          const u32x2 a = *reinterpret_cast<const u32x2*>(kp), b = *reinterpret_cast<const u32x2*>(vp);
 #pragma unroll
-            for (int i = 0; i < LW; ++i) { f.k[h][i] = a[i]; f.v[h][i] = b[i]; }
-          }
-          f.kf[h] = c.ks[row * (D / kKv4Block) + g * D / 128];
-          f.vf[h] = c.vs[row * (D / kKv4Block) + g * D / 128];
-        } else {       // past the end, or no such page: nothing that any row sees, and zeros where P = 0 meets V
-#pragma unroll
-          for (int i = 0; i < LW; ++i) f.k[h][i] = f.v[h][i] = 0;
-          f.kf[h] = page < 0 ? 256u : 127u;
-          f.vf[h] = 127u;
+          for (int i = 0; i < LW; ++i) { f.k[h][i] = a[i]; f.v[h][i] = b[i]; }
         }
+      }
+      // the factor bytes of all 32 keys' K and V rows in one load: 16 lanes each for K keys 0.., 16.., V keys 0.., 16..
+      // (addresses chosen as integers: a select of pointers would be a load of unknown address space, which the LDS
+      // counter waits for too)
+      const uint64_t addr = (lane & 32 ? (uint64_t)c.vs : (uint64_t)c.ks) + ((lane & 16) ? row[1] : row[0]) * (D / kKv4Block) +
+                            (uint32_t)(li * (D / kKv4Block));
+      if constexpr (D == 128) f.factors = *reinterpret_cast<const __attribute__((address_space(1))) uint32_t*>(addr);
+      else f.factors = *reinterpret_cast<const __attribute__((address_space(1))) uint16_t*>(addr);
+    };
+    // The factor byte of this lane's block of K and of V, for both halves: each row of 16 lanes to all rows, then the block's byte
+    auto unpack = [&](uint32_t w, uint32_t (&kf)[2], uint32_t (&vf)[2]) {
+      const auto x = __builtin_amdgcn_permlane32_swap(w, w, false, false);      // rows {0, 1, 0, 1}, {2, 3, 2, 3}
+      const auto k2 = __builtin_amdgcn_permlane16_swap(x[0], x[0], false, false);
+      const auto v2 = __builtin_amdgcn_permlane16_swap(x[1], x[1], false, false);
+      const int shift = 8 * (g * D / 128);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        kf[h] = (k2[h] >> shift) & 255u;
+        vf[h] = (v2[h] >> shift) & 255u;
       }
     };
 
-    Fetch cur, nxt;
-    fetch(b0, cur);
-    for (int blk = b0; blk < b1; ++blk) {
-      if (blk + 1 < b1) fetch(blk + 1, nxt);
+    auto step = [&](int blk, const Fetch& cur) {
       const int j0 = blk * kKvBlockKeys + wave * kKvStep;
+      uint32_t kf[2], vf[2];
+      unpack(cur.factors, kf, vf);
+      // what no row sees has finite values (its weight is 0): places past the end, halves without a page
+      if (j0 + kKvStep > keys || cur.gone) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          if (j0 + 16 * h + li >= keys || ((cur.gone >> h) & 1)) kf[h] = vf[h] = 127;
+      }
       // blocks that held a NaN or an infinity make the scores of their keys NaN and weigh nothing themselves
       uint32_t poison = 0, gone = 0;     // bits: keys of the 32
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint64_t bad = __builtin_amdgcn_ballot_w64(cur.kf[h] == kKv4Nan || cur.vf[h] == kKv4Nan);
+        uint64_t bad = __builtin_amdgcn_ballot_w64(kf[h] == kKv4Nan || vf[h] == kKv4Nan);
         if (bad) {
           bad |= bad >> 32;
           bad |= bad >> 16;
           poison |= (uint32_t)(bad & 0xffff) << (16 * h);
-          if (cur.kf[h] == kKv4Nan) cur.kf[h] = 127;
-          if (cur.vf[h] == kKv4Nan) cur.vf[h] = 127;
+          if (kf[h] == kKv4Nan) kf[h] = 127;
+          if (vf[h] == kKv4Nan) vf[h] = 127;
         }
-        if (__builtin_amdgcn_ballot_w64(cur.kf[h] == 256u) != 0) gone |= 0xffffu << (16 * h);
+        if ((cur.gone >> h) & 1) gone |= 0xffffu << (16 * h);
       }
       // ---- V: to bf16, through LDS
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < LW; ++i)
-          *reinterpret_cast<bf16x8*>(vt + tile_off<D>(16 * h + li, g * (D / 4) + 8 * i)) = kv4_values(cur.v[h][i], kv4_factor(cur.vf[h]));
+          *reinterpret_cast<bf16x8*>(vt + tile_off<D>(16 * h + li, g * (D / 4) + 8 * i)) = kv4_values(cur.v[h][i], kv4_factor(vf[h]));
       // ---- S^T = K Q^T: lane holds row li of the queries, keys 4g .. 4g+3 of each 16
       f32x4 sc[R][2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const bf16x8 ka = kv4_values(cur.k[h][ks], kv4_factor(cur.kf[h] & 255u));
+          const bf16x8 ka = kv4_values(cur.k[h][ks], kv4_factor(kf[h]));
 #pragma unroll
           for (int rt = 0; rt < R; ++rt)
             sc[rt][h] = mfma16(ka, qreg[rt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : sc[rt][h]);
@@ -293,7 +332,25 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      cur = nxt;
+    };
+    // Two sets of registers in turn (copied from one to the other, a fetch would be waited for at the copy), and a fetch on every
+    // path (at the end of the last block again), so that what is waited for is the older one only.
+    auto ask = [&](int blk, Fetch& f) {
+      blk = min(blk, b1 - 1);
+      if (blk - pages_at == 32) take_pages(blk);
+      fetch(blk, f);
+    };
+    if (c.n_pages > 0) {       // (a cache without pages has no memory at all)
+      Fetch even, odd;
+      take_pages(b0);
+      fetch(b0, even);
+      for (int blk = b0; blk < b1; blk += 2) {
+        ask(blk + 1, odd);
+        step(blk, even);
+        if (blk + 1 >= b1) break;
+        ask(blk + 2, even);
+        step(blk + 1, odd);
+      }
     }
 
     // ---- join the four wavefronts, one row tile at a time
@@ -348,26 +405,29 @@ void kv4_attn_kernel(const char* __restrict__ q, const Kv4Table t, const Kv4Cach
 }
 
 // Joins the pieces of every unit that more than one workgroup worked on, and writes the rows of sequences that have nothing
-// to look at.  blockIdx.x: (unit, row of its row block); units as in the line: sequence, K/V head, row block.
+// to look at.  blockIdx.x: output row, token-major, head-minor.  D / 4 threads share a piece, four pieces each at a time.
 template <int D>
 __global__ __launch_bounds__(kKvThreads) void kv4_join_kernel(const Kv4Table t, const Kv4Cache c, const Kv4Shape sh, int pieces,
                                                               __bf16* __restrict__ out, float* __restrict__ lse,
-                                                              const float* __restrict__ slots) {
+                                                              const char* __restrict__ workspace) {
   constexpr int TPP = D / 4, PAR = kKvThreads / TPP;     // threads per piece, pieces at a time
-  __shared__ long long before[VFM_MAX_SEQS + 1], part[kKvWaves];
+  constexpr int kAtOnce = 4;
   __shared__ float red[PAR][D + 1], redm[PAR];
-  const long long total = kv4_scan(t, c, sh, before, part);
-  const long long per = (total + pieces - 1) / pieces;
-
-  // output row blockIdx.x: token-major, head-minor
+  const float* slots = reinterpret_cast<const float*>(workspace + kKvHead);
+  const long long* before = reinterpret_cast<const long long*>(workspace);
   const int tok_all = t.cu[0] + blockIdx.x / sh.n_heads, head = blockIdx.x % sh.n_heads;
-  const int s = kv4_seq_of(t, tok_all);
+  const int tid = threadIdx.x, lane = tid & 63;
+  int s = -1;                                            // the last sequence that begins at or before the token
+#pragma unroll
+  for (int i = 0; i < VFM_MAX_SEQS; i += 64) s += __builtin_popcountll(__builtin_amdgcn_ballot_w64(i + lane < t.n && t.cu[i + lane] <= tok_all));
+  s = __builtin_amdgcn_readfirstlane(s);
   const int q0 = t.cu[s], nq = t.cu[s + 1] - q0, tok = tok_all - q0;
   const int keys = kv4_keys(c, c.lens[s], nq);
+  const long long total = before[VFM_MAX_SEQS], first = before[s];
+  const long long per = (total + pieces - 1) / pieces;
   const int kvh = head / sh.group, row = tok * sh.group + head - kvh * sh.group;
   __bf16* op = out + ((size_t)tok_all * sh.n_heads + head) * D;
   float* lp = lse + (size_t)head * sh.total + tok_all;
-  const int tid = threadIdx.x;
   if (keys == 0) {
     if (tid < D) op[tid] = (__bf16)0.f;
     if (tid == 0) *lp = -INFINITY;
@@ -375,24 +435,43 @@ __global__ __launch_bounds__(kKvThreads) void kv4_join_kernel(const Kv4Table t, 
   }
   const int nb = (keys + kKvBlockKeys - 1) / kKvBlockKeys;
   const int n_rb = kv4_row_blocks(nq, sh), rblk = row / sh.rb_rows, rr = row - rblk * sh.rb_rows;
-  const long long u0 = before[s] + (long long)(kvh * n_rb + rblk) * nb, u1 = u0 + nb;
+  const long long u0 = first + (long long)(kvh * n_rb + rblk) * nb, u1 = u0 + nb;
   const int p0 = (int)(u0 / per), p1 = (int)((u1 - 1) / per);
   if (p0 == p1) return;                                  // one workgroup had all of it
-  auto slot = [&](int p) {                               // the unit is the piece's second, last one where it begins inside the piece
-    const bool inside = p == p0 && u0 > (long long)p * per;
-    return slots + (size_t)(2 * p + (inside ? 1 : 0)) * kv4_slot_floats<D>(sh.rb_rows);
-  };
   const int sub = tid / TPP, col = (tid % TPP) * 4;
   float m = kKvUnset, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p = p0 + sub; p <= p1; p += PAR) {
-    const float* sp = slot(p);
-    const float pm = sp[2 * rr], pl = sp[2 * rr + 1];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(sp + 2 * sh.rb_rows + rr * D + col);
-    const float mn = fmaxf(m, pm), a = fast_exp2(m - mn), b = fast_exp2(pm - mn);
+  for (int p = p0 + sub; p <= p1; p += PAR * kAtOnce) {
+    float pm[kAtOnce], pl[kAtOnce];
+    f32x4 v[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int x = p + i * PAR;
+      pm[i] = kKvUnset;
+      pl[i] = 0.f;
+      v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (x <= p1) {
+        // the unit is the piece's second, last one where it begins inside the piece
+        const bool inside = x == p0 && u0 > (long long)x * per;
+        const float* sp = slots + (size_t)(2 * x + (inside ? 1 : 0)) * kv4_slot_floats<D>(sh.rb_rows);
+        pm[i] = sp[2 * rr];
+        pl[i] = sp[2 * rr + 1];
+        v[i] = *reinterpret_cast<const f32x4*>(sp + 2 * sh.rb_rows + rr * D + col);
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) mn = fmaxf(mn, pm[i]);
+    const float a = fast_exp2(m - mn);
     m = mn;
-    l = l * a + pl * b;
-    acc = acc * a + v * b;
+    l *= a;
+    acc *= a;
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const float b = fast_exp2(pm[i] - mn);
+      l += pl[i] * b;
+      acc += v[i] * b;
+    }
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) red[sub][col + i] = acc[i];
@@ -432,7 +511,7 @@ size_t kv4_attn_workspace(const int32_t* cu, int n_seqs, int n_heads, int n_kv_h
     const size_t need = (size_t)2 * pieces_of(head_dim, r) * 16 * r * (head_dim + 2) * sizeof(float);
     most = need > most ? need : most;
   }
-  return most;
+  return most == 0 ? 0 : kKvHead + most;
 }
 
 hipError_t launch_kv4_attn(const void* q, uint32_t q_row, const Kv4Table& t, const Kv4Cache& c, int n_heads, int total,
@@ -448,10 +527,10 @@ hipError_t launch_kv4_attn(const void* q, uint32_t q_row, const Kv4Table& t, con
     return r == 1 ? kv4_attn_kernel<D, 1> : r == 2 ? kv4_attn_kernel<D, 2> : kv4_attn_kernel<D, 4>;
   };
   auto kern = head_dim == 128 ? pick(IntC<128>{}) : pick(IntC<64>{});
-  hipError_t e = launch(kern, dim3(pieces), dim3(kKvThreads), 0, stream, (const char*)q, t, c, sh, (__bf16*)out, lse, (float*)workspace);
+  hipError_t e = launch(kern, dim3(pieces), dim3(kKvThreads), 0, stream, (const char*)q, t, c, sh, (__bf16*)out, lse, (char*)workspace);
   if (e != hipSuccess) return e;
   auto join = head_dim == 128 ? kv4_join_kernel<128> : kv4_join_kernel<64>;
-  return launch(join, dim3(rows_out), dim3(kKvThreads), 0, stream, t, c, sh, pieces, (__bf16*)out, lse, (const float*)workspace);
+  return launch(join, dim3(rows_out), dim3(kKvThreads), 0, stream, t, c, sh, pieces, (__bf16*)out, lse, (const char*)workspace);
 }
 
 }  // namespace vfm

@@ -350,3 +350,49 @@ def test_a_prompt_in_chunks_then_tokens(hd):
         assert U.rel_rms(U.to_f64(out), U.to_f64(o2)) <= U.TOL_OUT_RELRMS
         have = [a + b_ for a, b_ in zip(have, new)]
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_lengths_far_past_the_table(hd):
+    """A sequence whose length no table holds: its new tokens see the whole table and are not kept themselves."""
+    b = _binding()
+    lens, new, kvh = (2 ** 31 - 1, 2 ** 31 - 2, 60, 2 ** 30), (3, 1, 2, 40), 2
+    c = Cache((60, 20, 64, 33), kvh, hd, 16, seed=30)
+    room = c.table.shape[1] * 16
+    for s, n in enumerate((4, 2, 4, 3)):            # (tables shorter than the widest one end in -1)
+        assert (c.table[s] >= 0).sum() == n and room == 64
+    _fill(c, (60, 20, 62, 33), 31)
+    for t in c.bufs[2:]:
+        t.clamp_(max=130)
+    before = [t.clone() for t in c.bufs]
+    k, v = (U.to_device(_bits(32, n, (sum(new), kvh, hd))) for n in ("k", "v"))
+    b.vfm_kv4_append(k, v, *c.bufs, c.pages, _dev_i32(lens), _cu(new))
+    changed = np.zeros((before[0].shape[0], 16), dtype=bool)
+    for t, old in zip(c.bufs, before):
+        changed |= (t != old).any(dim=3).any(dim=1).cpu().numpy()
+    want = np.zeros_like(changed)
+    want[c.table[2, 60 // 16], [60 % 16, 61 % 16]] = True
+    assert np.array_equal(changed, want)
+    _attend(c, U.to_device(_bits(33, "q", (sum(new), 4, hd))), lens, _cu(new))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_sequences_that_share_pages(hd):
+    """Two sequences with one prompt's pages in common and ends of their own; one call's table, two streams in turn."""
+    import torch
+    b = _binding()
+    c = Cache((96, 40, 8), 2, hd, 32, seed=34)
+    _fill(c, (96, 40, 8), 35)
+    for t in c.bufs[2:]:
+        t.clamp_(max=130)
+    c.table[1, :3] = c.table[0, :3]
+    c.table[1, 2] = c.table[2, 0]                   # 64 places of the first one's, then the third's page
+    c.pages.copy_(torch.from_numpy(c.table))
+    lens, new = (90, 66, 5), (2, 4, 1)
+    q = U.to_device(_bits(36, "q", (sum(new), 6, hd)))
+    out, lse = _attend(c, q, lens, _cu(new))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = b.vfm_kv4_attn(q, *c.bufs, c.pages, _dev_i32(lens), _cu(new), hd ** -0.5, stream=side)
+    side.synchronize()
+    assert torch.equal(out, got[0]) and torch.equal(lse, got[1])
