@@ -10,6 +10,7 @@
 //   dkdv : a workgroup owns 128 keys and walks the rows that see any of them.
 // S and dP are formed in both (7 products instead of 5): sums of dQ over key tiles would need device-wide atomics, which are
 // executed at the memory side on this chip.
+#include "cattn_careful.h"
 #include "cattn_common.h"
 #include "cattn_dkdv.h"
 #include "cattn_dq.h"
@@ -187,6 +188,8 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
     }
     wait_vmcnt<0>();
     __syncthreads();
+    if (any_nan(dqacc))       // (rare; values that are not seen take no part: see the mask)
+      dq_checked<D>(dqacc, q, k, v, dout, cs, shape_anew(sh), kvh, row_w, kg, KG, n_tiles * Cfg::kBC, false, lse2, dlt);
   }
   if constexpr (KG > 1) {
     auto sums = [&](int x) { return reinterpret_cast<f32x4*>(smem + Cfg::kTurn) + (size_t)((x - 1) * (4 / KG) + rw) * (8 * D); };

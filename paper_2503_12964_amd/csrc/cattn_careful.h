@@ -1,0 +1,160 @@
+// Keys and rows that hold a NaN or an infinity, for those that do not see them.  Included by the causal attention kernels.
+//
+// A pair (row, key) that is not seen has weight 0 in the second products, but 0 times a NaN or an infinity is a NaN.  The only
+// such pairs that are multiplied at all lie in the units that cross the diagonal, or next to it in a wavefront's tile.  To look at
+// their operands would cost the loops; so every wavefront looks at its sums once, at the end.  Where they hold a NaN, and what its
+// rows do not all see holds something that is not finite, it forms its sums again: pair by pair from memory, with
+// plain multiplications, over the pairs that are seen.  That is slow, a microsecond or so per key or row, and met only by such inputs.
+// The look itself (an addition per sum) and the code beside the loops cost a call about 1 % (8,000 tokens x 16/1 heads x 128, backward:
+// 860 us without, 868 with; at head_dim 64 nothing measurable but in the cut forward, 4,000 x 8/2: 56.6, 61.5).
+#pragma once
+
+#include "cattn_common.h"
+
+namespace vfm {
+
+// A wave-uniform value that the compiler takes for a new one: what is rarely needed is worked out from it where it is needed, and
+// nothing of that is kept in registers through the loops.
+__device__ __forceinline__ int anew(int x) {
+  x = __builtin_amdgcn_readfirstlane(x);
+  asm volatile("" : "+s"(x));
+  return x;
+}
+__device__ __forceinline__ CausalShape shape_anew(const CausalShape& sh) {
+  CausalShape s = sh;
+  s.group = anew(s.group);
+  s.n_kv_heads = anew(s.n_kv_heads);
+  return s;
+}
+
+template <int N>
+__device__ __forceinline__ bool any_nan(const f32x16 (&a)[N]) {   // in any lane (sums that overflow count too)
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e & 3] += a[i][e];
+  const float t = (s[0] + s[1]) + (s[2] + s[3]);
+  return __builtin_amdgcn_ballot_w64(t != t) != 0;
+}
+template <int N>
+__device__ __forceinline__ bool only_nan(const f32x16 (&a)[N]) {  // in every lane
+  bool all = true;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) all &= a[i][e] != a[i][e];
+  return __builtin_amdgcn_ballot_w64(!all) == 0;
+}
+__device__ __forceinline__ bool not_finite(u32x4 w) {             // any of eight bf16
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+// Whether rows [r0, r1) hold anything that is not finite; at(r): address of row r.  The whole wavefront asks.
+template <int D, class At>
+__device__ __forceinline__ bool rows_not_finite(int r0, int r1, At at) {
+  constexpr int CPR = D / 8;
+  const int lane = lane_anew();
+  bool bad = false;
+#pragma unroll 1
+  for (int r = r0 + lane / CPR; r < r1; r += 64 / CPR)
+    bad |= not_finite(*reinterpret_cast<const u32x4*>(at(r) + lane % CPR * 16));
+  return __builtin_amdgcn_ballot_w64(bad) != 0;
+}
+// This lane's half (elements 16 ks + 8 g + e) of the product of two rows, summed with the other half's
+template <int D>
+__device__ __forceinline__ float row_dot(const char* a, const char* b) {
+  float s = 0.f;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(a + ks * 32), y = *reinterpret_cast<const bf16x8*>(b + ks * 32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf((float)x[e], (float)y[e], s);
+  }
+  return pair_sum(s);
+}
+// acc += w * row, as the accumulators lie (elements 32 db + 8 q + 4 g + e; row: this lane's first, 4 g)
+template <int D>
+__device__ __forceinline__ void add_row(f32x16 (&acc)[D / 32], float w, const char* row) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const bf16x4 x = *reinterpret_cast<const bf16x4*>(row + db * 64 + q4 * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[db][4 * q4 + e] = __builtin_fmaf(w, (float)x[e], acc[db][4 * q4 + e]);
+    }
+}
+template <int D>
+__device__ __forceinline__ void clear(f32x16 (&acc)[D / 32]) {
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+}
+
+// The first key that not all rows of a wavefront see, at the latest the last key (keys past it are copies of it); wave_min: the last
+// that its first row sees.
+__device__ __forceinline__ int first_unseen(int wave_min, int last_key) {
+  const int j = wave_min < 0 ? 0 : wave_min + 1;
+  return j < last_key ? j : last_key;
+}
+
+// out's sums of 32 rows over keys [j0, j1).  q_row: this lane's; k, v: the sequence's first; lim: last key that the row sees; m: the
+// reference that the sum of its exponentials has.
+template <int D>
+__device__ __forceinline__ void fwd_again(f32x16 (&acc)[D / 32], const char* q_row, const char* k, uint32_t k_row, const char* v,
+                                          uint32_t v_row, int j0, int j1, int lim, float m, float scale_log2) {
+  const int g = lane_anew() >> 5;
+  clear<D>(acc);
+#pragma unroll 1
+  for (int j = j0; j < j1; ++j) {
+    const float s = row_dot<D>(q_row + 16 * g, k + (size_t)j * k_row + 16 * g);
+    if (j <= lim) add_row<D>(acc, fast_exp2(s * scale_log2 - m), v + (size_t)j * v_row + 8 * g);
+    if ((j & 31) == 31 && only_nan(acc)) break;
+  }
+}
+
+// dq's sums of 32 rows over the 32-key blocks b0, b0 + step .. below key j1.
+template <int D>
+__device__ __forceinline__ void dq_again(f32x16 (&acc)[D / 32], const char* q_row, const char* do_row, const char* k, uint32_t k_row,
+                                         const char* v, uint32_t v_row, int b0, int step, int j1, int lim, float lse2, float delta,
+                                         float scale_log2) {
+  const int g = lane_anew() >> 5;
+  clear<D>(acc);
+#pragma unroll 1
+  for (int j = 32 * b0; j < j1; j += (j & 31) == 31 ? 32 * step - 31 : 1) {
+    const char* kj = k + (size_t)j * k_row;
+    const float s = row_dot<D>(q_row + 16 * g, kj + 16 * g), dp = row_dot<D>(do_row + 16 * g, v + (size_t)j * v_row + 16 * g);
+    if (j <= lim) add_row<D>(acc, fast_exp2(s * scale_log2 - lse2) * (dp - delta), kj + 8 * g);
+    if ((j & 31) == 31 && only_nan(acc)) break;
+  }
+}
+
+// dk's and dv's sums of 32 keys over the rows of the 32-row blocks that take(block) takes, from r1 - 1 back to r0.  k_row, v_row: this
+// lane's key; q_at(r), do_at(r), stat_at(r): addresses of row r and index of its statistics; row_min: the first row that sees the key.
+template <int D, class Take, class QAt, class DoAt, class StatAt>
+__device__ __forceinline__ void dkdv_again(f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32], const char* k_row, const char* v_row, int r0, int r1,
+                                           Take take, QAt q_at, DoAt do_at, StatAt stat_at, const float* lse2, const float* delta,
+                                           int row_min, float scale_log2) {
+  const int g = lane_anew() >> 5;
+  clear<D>(dk);
+  clear<D>(dv);
+#pragma unroll 1
+  for (int r = r1 - 1; r >= r0; --r) {
+    if (!take(r >> 5)) { r &= ~31; continue; }
+    const char *qr = q_at(r), *dr = do_at(r);
+    const size_t at = stat_at(r);
+    const float s = row_dot<D>(qr + 16 * g, k_row + 16 * g), dp = row_dot<D>(dr + 16 * g, v_row + 16 * g);
+    if (r >= row_min) {
+      const float p = fast_exp2(s * scale_log2 - lse2[at]);
+      add_row<D>(dk, p * (dp - delta[at]), qr + 8 * g);
+      add_row<D>(dv, p, dr + 8 * g);
+    }
+    if ((r & 31) == 0 && only_nan(dk) && only_nan(dv)) break;
+  }
+}
+
+}  // namespace vfm

@@ -21,6 +21,7 @@
 //  - Scores of pairs that are not seen become -inf before their exponentials, in the blocks that cross the diagonal only.
 #pragma once
 
+#include "cattn_careful.h"
 #include "cattn_common.h"
 
 namespace vfm {
@@ -52,6 +53,76 @@ struct CKvCfg {
   static constexpr int kLoadsPerWave = kBQ * kChunksPerRow / (kCBwdWaves * 64);
 };
 
+// The row that is the first to see key j
+__device__ __forceinline__ int first_row_of(const CausalSeq& cs, int group, int j) {
+  const long long r = ((long long)j - cs.off) * group;
+  return r < 0 ? 0 : r > 0x7fffffffLL ? 0x7fffffff : (int)r;
+}
+// What a workgroup takes: a sequence's first keys, which most rows see, first.
+struct KvWalk {
+  CausalSeq cs;
+  int kvh, split, j0;     // first key
+  int rt0, n_tiles;       // rows: n_tiles tiles from rt0 on
+};
+template <int D, int RG>
+__device__ __forceinline__ KvWalk kv_walk(int block, const XSegTable& segs, const TileIndex& ti, const CausalShape& sh, int splits) {
+  constexpr int kBQ = CKvCfg<D, RG>::kBQ;
+  KvWalk w;
+  w.kvh = block % sh.n_kv_heads;
+  int seq, tk;
+  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, block / sh.n_kv_heads / splits, seq, tk);
+  w.split = block / sh.n_kv_heads % splits;
+  w.cs = causal_seq(segs, seq, sh.group);
+  w.j0 = tk * CKvCfg<D, RG>::kBC;
+  w.rt0 = first_row_of(w.cs, sh.group, w.j0) / kBQ * kBQ;
+  w.n_tiles = w.rt0 < w.cs.rows ? (w.cs.rows - w.rt0 + kBQ - 1) / kBQ : 0;
+  if (splits > 1) {
+    const int t0 = (int)((long long)w.n_tiles * w.split / splits), t1 = (int)((long long)w.n_tiles * (w.split + 1) / splits);
+    w.rt0 += t0 * kBQ;
+    w.n_tiles = t1 - t0;
+  }
+  return w;
+}
+
+// A wavefront's sums hold a NaN: from rows that only some of its keys are seen by?
+template <int D, int RG>
+__device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32], int wave, const __bf16* q, const __bf16* k,
+                                             const __bf16* v, const __bf16* dout, const float* lse2, const float* delta,
+                                             const XSegTable& segs, const TileIndex& ti, const CausalShape& sh, int splits) {
+  constexpr int RB = D * 2, kBQ = CKvCfg<D, RG>::kBQ;
+  const KvWalk w = kv_walk<D, RG>(anew(blockIdx.x), segs, ti, sh, splits);
+  const CausalSeq& cs = w.cs;
+  const int rg = wave / (kCBwdWaves / RG), jw = w.j0 + wave % (kCBwdWaves / RG) * 32;
+  const int row0 = first_row_of(cs, sh.group, jw), r_first = row0 <= w.rt0 ? w.rt0 : row0 / kBQ * kBQ;
+  const int r_end = min(w.rt0 + w.n_tiles * kBQ, cs.rows), r_some = min(first_row_of(cs, sh.group, jw + 31), r_end);
+  auto row_at = [&](const __bf16* base, size_t row_bytes, int r) {
+    const int tok = r / sh.group;
+    return (const char*)base + (size_t)(cs.qs + tok) * row_bytes + (size_t)(w.kvh * sh.group + r - tok * sh.group) * RB;
+  };
+  auto q_at = [&](int r) { return row_at(q, sh.q_row, r); };
+  auto do_at = [&](int r) { return row_at(dout, (size_t)sh.n_heads * RB, r); };
+  auto stat_at = [&](int r) {
+    const int tok = r / sh.group;
+    return (size_t)(w.kvh * sh.group + r - tok * sh.group) * sh.total_q + cs.qs + tok;
+  };
+  bool bad = rows_not_finite<D>(r_first, r_some, q_at) || rows_not_finite<D>(r_first, r_some, do_at);
+  if (!bad) {
+    bool nan = false;
+#pragma unroll 1
+    for (int r = r_first + lane_anew(); r < r_some; r += 64) {
+      const float a = lse2[stat_at(r)], b = delta[stat_at(r)];
+      nan |= a != a || b != b;
+    }
+    bad = __builtin_amdgcn_ballot_w64(nan) != 0;
+  }
+  if (!bad) return;
+  const int key = min(jw + (lane_anew() & 31), cs.kl - 1);
+  dkdv_again<D>(dk, dv, (const char*)k + (size_t)(cs.ks + key) * sh.k_row + (size_t)w.kvh * RB,
+                (const char*)v + (size_t)(cs.ks + key) * sh.v_row + (size_t)w.kvh * RB, r_first, r_end,
+                [&](int block) { return RG == 1 || block % RG == rg; }, q_at, do_at, stat_at, lse2, delta,
+                first_row_of(cs, sh.group, key), sh.scale_log2);
+}
+
 template <int D, int RG>
 __global__ __launch_bounds__(kCBwdWaves * 64, D == 64 && RG < 4 ? 2 : 1)
 void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
@@ -70,12 +141,9 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
 
   extern __shared__ __attribute__((aligned(16))) char smem[];
 
-  const int kvh = blockIdx.x % sh.n_kv_heads;
-  int seq, tk;
-  locate_tile_wave<VFM_MAX_XSEQS>(ti.cu, segs.n, blockIdx.x / sh.n_kv_heads / splits, seq, tk);   // a sequence's first keys, which most rows see, first
-  const int split = blockIdx.x / sh.n_kv_heads % splits;
-  const CausalSeq cs = causal_seq(segs, seq, sh.group);
-  const int j0 = tk * Cfg::kBC;
+  const KvWalk walk = kv_walk<D, RG>(blockIdx.x, segs, ti, sh, splits);
+  const int kvh = walk.kvh, split = walk.split, j0 = walk.j0, rt0 = walk.rt0, n_tiles = walk.n_tiles;
+  const CausalSeq cs = walk.cs;
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -89,19 +157,10 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     return reinterpret_cast<__bf16*>(reinterpret_cast<char*>(base) + (size_t)(cs.ks + jw) * row_bytes) + kvh * D;
   };
 
-  // row that is the first to see key j
-  auto first_row = [&](int j) {
-    const long long r = ((long long)j - cs.off) * sh.group;
-    return r < 0 ? 0 : r > 0x7fffffffLL ? 0x7fffffff : (int)r;
-  };
-  int rt0 = first_row(j0) / kBQ * kBQ;
-  int n_tiles = rt0 < cs.rows ? (cs.rows - rt0 + kBQ - 1) / kBQ : 0;
+  auto first_row = [&](int j) { return first_row_of(cs, sh.group, j); };
   // where this wavefront's sums go if the rows are split: 32 keys of dK, then of dV, as the accumulators lie
   f32x4* part = nullptr;
   if (splits > 1) {
-    const int t0 = (int)((long long)n_tiles * split / splits), t1 = (int)((long long)n_tiles * (split + 1) / splits);
-    rt0 += t0 * kBQ;
-    n_tiles = t1 - t0;
     // blocks of 32 keys, tile by tile (a sequence's last tile may have some past its end)
     const size_t block = (size_t)(blockIdx.x / sh.n_kv_heads / splits) * (Cfg::kBC / 32) + wave % (kCBwdWaves / RG);
     part = reinterpret_cast<f32x4*>(parts) + ((block * sh.n_kv_heads + kvh) * splits + split) * (16 * D);
@@ -434,6 +493,9 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
     }
   }
   idle_from(wave_tiles);
+
+  if (wave_tiles > 0 && (any_nan(dkacc) || any_nan(dvacc)))   // (rare)
+    dkdv_checked<D, RG>(dkacc, dvacc, wave, q, k, v, dout, lse2, delta, segs, ti, shape_anew(sh), splits);
 
   // ---- epilogue: dK (scaled) and dV of this wavefront's keys; each wavefront turns its tiles through a piece of the ring
   if constexpr (RG > 1) {

@@ -11,6 +11,7 @@
 // meeting the barriers for the wavefronts behind it), and row tiles are handed out longest first.
 #include <math.h>
 
+#include "cattn_careful.h"
 #include "cattn_common.h"
 
 namespace vfm {
@@ -37,6 +38,21 @@ constexpr int kSgcValu = 0x002, kSgcMfma = 0x008, kSgcDsRead = 0x100;
 
 // Wavefronts per SIMD
 constexpr int fwd_waves(int D, int W) { return W == 1 ? 1 : W == 2 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
+
+// A wavefront's sums over keys [j0, j1) hold a NaN: from values that only some of its rows see?
+template <int D>
+__device__ __forceinline__ void fwd_checked(f32x16 (&acc)[D / 32], const __bf16* q, const __bf16* k, const __bf16* v,
+                                            const CausalSeq& cs, const CausalShape& sh, int kvh, int row_w, int j0, int j1, float m) {
+  constexpr int RB = D * 2;
+  const char* kbase = (const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB;
+  const char* vbase = (const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB;
+  j1 = min(j1, cs.kl);
+  const int first = min(row_w, cs.rows - 1) / sh.group + cs.off;
+  if (!rows_not_finite<D>(max(first_unseen(first, cs.kl - 1), j0), j1, [&](int j) { return vbase + (size_t)j * sh.v_row; })) return;
+  const int row = min(row_w + (lane_anew() & 31), cs.rows - 1), tok = row / sh.group;
+  const char* q_row = (const char*)q + (size_t)(cs.qs + tok) * sh.q_row + (size_t)(kvh * sh.group + row - tok * sh.group) * RB;
+  fwd_again<D>(acc, q_row, kbase, sh.k_row, vbase, sh.v_row, j0, j1, tok + cs.off, m, sh.scale_log2);
+}
 
 // What a workgroup does of one tile: the units [u0, u1) of the keys that the tile's last row sees.  slot: null, or where the
 // unfinished results of a tile go that other workgroups share: per wavefront its accumulators as they lie (16 bytes a
@@ -357,6 +373,9 @@ void fwd_segment(const __bf16* __restrict__ q, const __bf16* __restrict__ k, con
   }
   for (int u = wave_units; u < n_units; ++u) idle_unit(u);
   wait_vmcnt<0>();   // no load may still be writing LDS when the workgroup ends
+
+  if (any_nan(oacc))     // (rare)
+    fwd_checked<D>(oacc, q, k, v, cs, shape_anew(sh), kvh, row_w, u0 * kCU, (u0 + wave_units) * kCU, m_run);
 
   if (slot) {
     float* o = slot + wave * (32 * D + 64);
