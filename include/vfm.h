@@ -420,12 +420,15 @@ VFM_API int vfm_attn_fwd_tile_rows(const int32_t* cu_seqlens, int n_seqs, int to
  * 8; the heads of a token are contiguous), so that they may be parts of one
  * projection's output; out: bf16 [total_q, n_heads, head_dim] and lse: fp32
  * [n_heads, total_q], contiguous, fully overwritten.  Both cu arrays are host
- * int32 [n_seqs+1].  One sequence's rows of a tensor span less than 4 GiB, and
- * total_q * n_heads <= 2^27 (SHAPE).  k and v may be NULL if total_kv is 0.
- * A query's results depend on no key that it does not see.  The result is
- * bitwise reproducible from run to run.
- * workspace: device, 256-byte aligned, vfm_cattn_fwd_workspace_size() bytes (0: none
- * needed, may be NULL).
+ * int32 [n_seqs+1].  One sequence's rows of a tensor span less than 4 GiB,
+ * total_q * n_heads <= 2^27 and total_kv * n_kv_heads <= 2^28 (SHAPE).  k and v may be
+ * NULL if total_kv is 0.  out and lse must not overlap the inputs.
+ * What a query or a key does not see has no part in its results, not even a NaN or an
+ * infinity there (but many of them cost time).  The result is bitwise reproducible from
+ * run to run; how a call is cut into pieces depends on all of its sizes and on the
+ * number of compute units, and with it the order in which the fp32 sums are formed.
+ * workspace: device, 256-byte aligned, vfm_cattn_fwd_workspace_size() bytes for the
+ * current device (0: none needed, may be NULL); its contents need not be initialised.
  * Errors: NULL, SHAPE, STRIDE, CU_SEQLENS, DTYPE, ALIGN, WORKSPACE, LAUNCH.
  */
 VFM_API size_t vfm_cattn_fwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,
@@ -442,9 +445,12 @@ VFM_API int vfm_cattn_fwd(const void* q, int64_t q_stride, const void* k, int64_
  * formulas of vfm_attn_bwd over the pairs that are seen; dk and dv are sums over
  * the query heads of the group.  dq of a query that sees no key and dk, dv of a
  * key that none sees are 0.  Each has a token stride of its own (as q, k, v).
- * All are fully overwritten and bitwise reproducible; they must not overlap the inputs.
+ * All are fully overwritten and bitwise reproducible; they must not overlap the inputs or
+ * one another (parts of one tensor with a stride are fine).  What a query or key does not see, and its
+ * workspace, as of vfm_cattn_fwd; the limits too.
  * Delta of a query that sees at most 32 keys is formed as sum_j P_ij (dout_i . v_j), as in
- * vfm_attn_bwd.  workspace: device, 256-byte aligned, vfm_cattn_bwd_workspace_size() bytes.
+ * vfm_attn_bwd.  workspace: device, 256-byte aligned, vfm_cattn_bwd_workspace_size() bytes
+ * (Delta and lse of every row, and the shares of cut sums).
  * Errors: NULL, SHAPE, STRIDE, CU_SEQLENS, DTYPE, ALIGN, WORKSPACE, LAUNCH.
  */
 VFM_API size_t vfm_cattn_bwd_workspace_size(const int32_t* cu_seqlens_q, const int32_t* cu_seqlens_kv, int n_seqs,

@@ -14,6 +14,7 @@
 #include "cattn_common.h"
 #include "cattn_dkdv.h"
 #include "cattn_dq.h"
+#include "cattn_plan.h"
 
 namespace vfm {
 
@@ -224,40 +225,6 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
 }
 
 // ---------------------------------------------------------------- launch
-// How the dK/dV pass is cut.  rg: wavefronts that share the keys of a workgroup (RG of cattn_dkdv_kernel): 1 where the workgroups of
-// 128 keys keep the chip busy; more where the longest of them, which walks all of its sequence's rows, takes longer than an
-// even share of the work.  splits: workgroups that share a key tile's rows, where that leaves the longest far longer still.
-// (Whole backward with rg = 1, 2, 4: head_dim 64: 2,146 and shorter x 12/4 heads 134, 101, 86 us; 6,000 x 16/4 463, 353, 370; 6,000 x
-// 32/8 609, 540, 659.  head_dim 128, rg = 1, 2: 2,000 x 16/4 227, 174; 3,000 + 2,500 x 24/8 357, 361; 6,000 x 32/8 956, 985.
-// Uncut and cut by share: head_dim 128: 1,000 x 8/2 75, 57; 2,000 x 16/4 158, 113; 4,000 x 16/4 327, 268; 8,000 x 16/1 1,918, 839;
-// 5,000 x 7/1 568, 235; 500 in two x 16/1 78, 47; head_dim 64, rg = 4
-// uncut and rg = 2 cut: 4,000 x 8/2 138, 101; 1,500 in three x 12/4 29, 34; in twice as many pieces 4,000 x 16/4 278,
-// 8,000 x 16/1 873.)
-struct KeysPlan { int rg, splits; };
-static KeysPlan keys_plan(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
-  long long longest = 0, work = 0, tiles_k = 0;    // in 64-row tiles of 128 keys
-  for (int s = 0; s < segs.n; ++s) {
-    const long long tiles = ((long long)segs.ql[s] * sh.group + 63) / 64, n = (segs.kl[s] + kCBwdBC - 1) / kCBwdBC;
-    // keys before the first query are seen by all rows, the others by half of them on average
-    const long long before = segs.kl[s] > segs.ql[s] ? (segs.kl[s] - segs.ql[s]) / kCBwdBC : 0;
-    longest = longest > tiles ? longest : tiles;
-    work += before * tiles + (n - before) * (tiles + 1) / 2;
-    tiles_k += n;
-  }
-  const long long share = work * sh.n_kv_heads / cus;
-  if (longest <= (head_dim == 64 ? share : share + share / 2) + 4) return {1, 1};
-  // about an even share of the work per piece, no shorter than kLeast tiles; at most eight workgroups per CU.  rg = 4 where a walk
-  // is too short to be cut
-  constexpr int kLeast = 14;
-  if (head_dim == 64 && longest > 3 * share && longest <= 4 * kLeast) return {4, 1};
-  const int rg = 2;
-  const long long piece = share > kLeast ? share : kLeast;
-  long long splits = (longest / rg + piece * 2 / 3) / piece;
-  const long long room = 8LL * cus / (tiles_k * rg * sh.n_kv_heads + 1);
-  splits = splits < room ? splits : room;
-  return {rg, (int)(splits < 2 ? 1 : splits > 16 ? 16 : splits)};
-}
-
 size_t cattn_bwd_parts(const XSegTable& segs, const CausalShape& sh, int head_dim) {
   const KeysPlan plan = keys_plan(segs, sh, head_dim, compute_unit_count());
   if (plan.splits == 1) return 0;
@@ -265,36 +232,6 @@ size_t cattn_bwd_parts(const XSegTable& segs, const CausalShape& sh, int head_di
   size_t blocks = 0;
   for (int s = 0; s < segs.n; ++s) blocks += (size_t)((segs.kl[s] + per - 1) / per) * (per / 32);
   return blocks * sh.n_kv_heads * plan.splits * 64 * head_dim * sizeof(float);
-}
-
-// Wavefronts that share the rows of a dQ workgroup (KG of cattn_dq_kernel).  A workgroup takes some us for its rows and results and
-// then its time per 64-key tile; the call takes as long as the longest of them or as all of them on the chip's CUs.  In us, as measured
-// at head_dim 128 with 256 rows (KG = 1), 64 and 32, and at 64 with 128, 64 and 32.  (Whole backward, KG = 1, 2, 4: head_dim 128:
-// 1,000 tokens x 8/2 heads 95, 84, 77; 2,000 x 16/4 174, 162, 184; 4,000 x 16/4 340, 384, 432; 256 queries x 4,096 keys x 16/4 138,
-// 101, 71; head_dim 64: 1,000 x 8/2 47, 44, 41; 4,000 x 8/2 154, 143, 168; 6,000 x 16/4 351, 359, 502.)
-static int dq_shares(const XSegTable& segs, const CausalShape& sh, int head_dim, int cus) {
-  struct Cost { int rows; float each, tile, busy, at_once; };   // per workgroup, per tile alone, per tile on a busy CU, on a CU at once
-  static const Cost costs[2][3] = {{{256, 6.f, 1.28f, 1.28f, 1.f}, {64, 6.7f, 0.64f, 0.64f, 1.f}, {32, 7.5f, 0.35f, 0.35f, 1.f}},
-                                   {{128, 6.f, 1.15f, 0.72f, 3.f}, {64, 6.7f, 0.6f, 0.4f, 2.f}, {32, 7.5f, 0.33f, 0.47f, 1.f}}};
-  int best = 0;
-  float least = 0.f;
-  for (int x = 0; x < 3; ++x) {
-    const Cost& c = costs[head_dim == 64][x];
-    long long longest = 0, groups = 0;
-    double work = 0.;
-    for (int s = 0; s < segs.n; ++s) {
-      const long long tiles = (segs.kl[s] + 63) / 64, n = ((long long)segs.ql[s] * sh.group + c.rows - 1) / c.rows;
-      const long long before = segs.kl[s] > segs.ql[s] ? (segs.kl[s] - segs.ql[s]) / 64 : 0;
-      if (n > 0) longest = longest > tiles ? longest : tiles;
-      groups += n;
-      work += (double)n * (before + (tiles - before + 1) / 2);
-    }
-    const float alone = c.each + longest * c.tile;
-    const float all = (float)((groups * (c.each / c.at_once) + work * c.busy) * sh.n_kv_heads / cus);
-    const float t = alone > all ? alone : all;
-    if (x == 0 || t < least) { least = t; best = x; }
-  }
-  return 1 << best;
 }
 
 template <int D>

@@ -23,11 +23,11 @@
 
 #include "cattn_careful.h"
 #include "cattn_common.h"
+#include "cattn_plan.h"
 
 namespace vfm {
 
 constexpr int kCBwdWaves = 4;
-constexpr int kCBwdBC = 128;   // keys per workgroup (RG = 1)
 constexpr int kSgbValu = 0x002, kSgbMfma = 0x008, kSgbDsRead = 0x100;
 
 template <int D, int RG>

@@ -9,14 +9,12 @@
 // a unit's exponentials would grow too large, K and V in rings of four LDS slots.  What the causal order adds: a wavefront masks only the
 // units that reach past its first row's limit, computes none past its last row's (it keeps fetching its share and
 // meeting the barriers for the wavefronts behind it), and row tiles are handed out longest first.
-#include <math.h>
-
 #include "cattn_careful.h"
 #include "cattn_common.h"
+#include "cattn_plan.h"
 
 namespace vfm {
 
-constexpr int kCU = 32;                 // keys per pipeline unit
 constexpr int kCRing = 4;               // LDS ring slots for K and for V
 constexpr float kCLog2e = 1.4426950408889634f;
 constexpr float kCLn2 = 0.6931471805599453f;
@@ -404,13 +402,6 @@ void fwd_segment(const __bf16* __restrict__ q, const __bf16* __restrict__ k, con
   store_tile_rows_at<D>(smem + wave * (32 * RB), oacc, inv, rows_valid, out_row);
 }
 
-// Units of the keys that the last row of tile tq sees
-__host__ __device__ inline int tile_units(int rows, int off, int group, int rows_per_tile, int tq) {
-  const int last = ((tq + 1) * rows_per_tile < rows ? (tq + 1) * rows_per_tile : rows) - 1;
-  const int keys = last / group + off + 1;
-  return keys > 0 ? (keys + kCU - 1) / kCU : 0;
-}
-
 // One workgroup per (K/V head, tile): all K/V heads of one tile before the next (heads on consecutive XCDs: an XCD keeps to
 // its heads), a sequence's last tile, which sees most, first.
 template <int D, int W>
@@ -428,84 +419,7 @@ void cattn_fwd_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
 }
 
 // ---------------------------------------------------------------- few tiles, many keys
-// A chunk of a prompt against a long past is fewer tiles than the chip has CUs, and each takes as long as the past is long.
-// Then every K/V head's line of units (tile after tile) is cut into equal pieces, one workgroup each.  A tile within a piece
-// is finished there; a cut tile's parts go to the workspace, and a second launch joins them in order.
-constexpr int kSplitSeqs = 32;          // the plan travels in 4 KB of kernel arguments
-constexpr int kSplitPieces = 768;
-constexpr int kSplitTile = 5;           // a tile's prologue and epilogue, as units
-constexpr int kSplitJoin = 10;          // the second launch, as units
-
-struct SplitPlan {
-  int n, pieces;
-  int qs[kSplitSeqs], ql[kSplitSeqs], ks[kSplitSeqs], kl[kSplitSeqs];
-  int cu[kSplitSeqs + 1];               // tiles of the sequences before
-  uint32_t start[kSplitPieces + 1];     // (tile << 16 | unit) where a piece begins; the last: where all end
-  __device__ __host__ int q_start(int s) const { return qs[s]; }
-  __device__ __host__ int q_len(int s) const { return ql[s]; }
-  __device__ __host__ int kv_start(int s) const { return ks[s]; }
-  __device__ __host__ int kv_len(int s) const { return kl[s]; }
-};
-
-// Cuts a run into pieces if that pays; false: it does not (or the plan cannot hold it).  In units (0.45 us with 128 rows, which
-// one workgroup per CU does at the chip's full rate): without, the run takes as long as its longest tile.  In pieces it takes work
-// / pieces and the traffic of the cuts, rows * head_dim * 8 bytes each out and back, which all pieces make at once: with as many
-// pieces as there is room (rows * head_dim / 2048 + 2) units per end of a piece.
-static bool make_split(const XSegTable& segs, const CausalShape& sh, int rows_per_tile, int head_dim, int slots, SplitPlan* plan) {
-  if (segs.n > kSplitSeqs || segs.n == 0) return false;
-  long long cost = 0;
-  int tiles = 0, longest = 0;
-  for (int s = 0; s < segs.n; ++s) {
-    const long long rows = (long long)segs.ql[s] * sh.group, n = (rows + rows_per_tile - 1) / rows_per_tile;
-    if (tiles + n > 0xffff || (tiles + n) * sh.n_kv_heads > 2LL * slots) return false;   // (enough of them)
-    for (int t = 0; t < n; ++t) {
-      const int u = tile_units((int)rows, segs.kl[s] - segs.ql[s], sh.group, rows_per_tile, t);
-      if (u > longest) longest = u;
-      cost += u + kSplitTile;
-    }
-    tiles += (int)n;
-  }
-  const int room = slots / sh.n_kv_heads < kSplitPieces ? slots / sh.n_kv_heads : kSplitPieces;
-  if (room < 2 || longest > 0xffff) return false;
-  const float ends = 2.f * (rows_per_tile * head_dim / 2048 + 2);
-  int pieces = (int)sqrtf((float)cost * room / ends);          // where work / pieces + ends * pieces / room is least
-  if (pieces > room) pieces = room;
-  if (pieces < 2 || (float)cost / pieces + ends * pieces / room + kSplitJoin > 0.8f * (longest + kSplitTile)) return false;
-  plan->n = segs.n;
-  int at = 0;
-  for (int s = 0; s <= kSplitSeqs; ++s) {
-    plan->cu[s] = at;
-    if (s == kSplitSeqs) break;
-    const bool live = s < segs.n;
-    plan->qs[s] = live ? segs.qs[s] : 0;
-    plan->ql[s] = live ? segs.ql[s] : 0;
-    plan->ks[s] = live ? segs.ks[s] : 0;
-    plan->kl[s] = live ? segs.kl[s] : 0;
-    if (live) at += (int)(((long long)segs.ql[s] * sh.group + rows_per_tile - 1) / rows_per_tile);
-  }
-  int p = 0;
-  long long before = 0;
-  plan->start[p++] = 0;
-  for (int s = 0, tile = 0; s < segs.n; ++s) {
-    const int rows = segs.ql[s] * sh.group, n = (rows + rows_per_tile - 1) / rows_per_tile;
-    for (int t = 0; t < n; ++t, ++tile) {
-      const int u = tile_units(rows, segs.kl[s] - segs.ql[s], sh.group, rows_per_tile, n - 1 - t);
-      for (; p < pieces; ++p) {
-        long long cut = cost * p / pieces - before - kSplitTile;   // in units of this tile
-        if (cut >= u - 2) break;                                   // (a part of one or two units is not worth its slot)
-        if (cut < 2) cut = 0;
-        const uint32_t at = (uint32_t)tile << 16 | (uint32_t)cut;
-        if (at <= plan->start[p - 1]) { plan->start[p] = plan->start[p - 1]; continue; }   // an empty piece
-        plan->start[p] = at;
-      }
-      before += u + kSplitTile;
-    }
-  }
-  for (; p <= pieces; ++p) plan->start[p] = (uint32_t)tiles << 16;
-  plan->pieces = pieces;
-  return true;
-}
-
+// The line of units that a piece is cut from: see make_split in cattn_plan.h.
 __device__ __forceinline__ void split_tile(const SplitPlan& plan, const CausalShape& sh, int rows_per_tile, int tile, int& seq, int& tq, int& units) {
   int t;
   locate_tile_wave<kSplitSeqs>(plan.cu, plan.n, tile, seq, t);
@@ -627,30 +541,6 @@ void cattn_fwd_join_kernel(__bf16* __restrict__ out, float* __restrict__ lse, co
   for (int q4 = 0; q4 < 4; ++q4)
     *reinterpret_cast<bf16x4*>(dst + 8 * q4) = to_bf16x4(f32x4{o[4 * q4], o[4 * q4 + 1], o[4 * q4 + 2], o[4 * q4 + 3]} * inv);
 }
-
-// Rows of a workgroup's tile.  256 where keys are many, for half the K/V traffic per product, if the chip is full of such
-// tiles or of long pieces of them; else 128, whose units take half as long.  No more than the longest sequence has, down to 32 (a
-// token or two against many keys: a wavefront without rows only takes LDS).  Measured at head_dim 128, 256 and 128 rows: 2,000 tokens x
-// 16/4 heads 50 and 37 us, 4,000 98 and 83, 6,000 x 32/8 284 with 256; in pieces 512 + 130 queries x 18,432 + 7,001 keys x 32/8
-// 179 and 225, 8,000 tokens x 2/1 69 and 89, 64 queries x 30,000 keys x 32/8 57 and 52.
-static int causal_rows(const XSegTable& segs, const CausalShape& sh, int head_dim) {
-  int longest = 0;
-  long long rows = 0, tiles = 0, units = 0;
-  for (int s = 0; s < segs.n; ++s) {
-    const long long r = (long long)segs.ql[s] * sh.group, n = (r + 255) / 256;
-    longest = longest > segs.kl[s] ? longest : segs.kl[s];
-    rows = rows > r ? rows : r;
-    tiles += n;
-    units += n * (segs.kl[s] - segs.ql[s] / 2) / kCU;
-  }
-  if (rows <= 64) return rows <= 32 ? 32 : 64;
-  const int cus = compute_unit_count();
-  if (head_dim == 64 || longest <= 1024) return 128;
-  const long long share = units * sh.n_kv_heads / cus;   // units per CU, were they dealt evenly; split if the longest tile has many more
-  return tiles * sh.n_kv_heads >= cus || (share >= 30 && longest / kCU * 2 >= 5 * share) ? 256 : 128;
-}
-// Workgroups that a split call is cut for
-static int causal_slots(int rows) { return compute_unit_count() * (rows <= 64 ? 2 : 1); }
 
 size_t cattn_fwd_workspace(const XSegTable& segs, const CausalShape& sh, int head_dim) {
   SplitPlan plan;

@@ -16,7 +16,8 @@ using vfm::XSegTable;
 
 constexpr long long kMaxRows = 1LL << 27;      // (token, head) rows: fewer than 2^32 threads in every launch, 32-bit byte offsets into lse
 constexpr long long kMaxFewRows = 1LL << 22;   // the same of vfm_kv4_attn, whose join takes 256 threads a row
-constexpr long long kMaxSpan = 0xffffffffLL;   // bytes of one sequence's rows of a tensor, likewise
+constexpr long long kMaxKeyRows = 1LL << 28;   // (key, K/V head) rows, likewise
+constexpr long long kMaxSpan = 0xffffffffLL;   // bytes of one sequence's rows of a tensor, for 32-bit offsets
 constexpr long long kSlack = 512;              // rows that a kernel's running offset goes past a sequence's end
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -49,7 +50,7 @@ int check_span(const int32_t* cu, int n_seqs, int64_t stride) {
 int check_causal(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, int total_q, int total_kv, int n_heads,
                  int n_kv_heads, int head_dim) {
   int st = check_heads(n_seqs, total_q, n_heads, n_kv_heads, head_dim);
-  if (!st && total_kv < 0) st = VFM_ERR_SHAPE;
+  if (!st && (total_kv < 0 || (long long)total_kv * n_kv_heads > kMaxKeyRows)) st = VFM_ERR_SHAPE;
   if (!st) st = check_cu(cu_q, n_seqs, total_q);
   if (!st) st = check_cu(cu_kv, n_seqs, total_kv);
   return st;

@@ -172,3 +172,18 @@ def test_wrappers_refuse_what_the_kernels_would_misread(lib, monkeypatch):
         B.vfm_kv4_append(q, q, *cache, pages, lens, cu, stream=0)        # four heads into a cache of two
     with pytest.raises(ValueError):
         B.vfm_kv4_gather(*cache, pages, cu, k=_dev(7, 2, 64), v=k, stream=0)
+
+
+def test_more_key_rows_than_a_launch_takes(lib):
+    change = dict(tk=1 << 20, ck=[0, 1 << 20], H=512, Hk=512, qs=512 * 128, ks=512 * 128, vs=512 * 128, D=128, tq=8)
+    assert _fwd(lib, **change) == SHAPE and _bwd(lib, **change) == SHAPE
+
+
+def test_a_cut_forward_asks_for_its_workspace(lib):
+    """One chunk against a long past is cut: without the workspace that it names it is refused."""
+    cq, ck = np.array([0, 64], dtype=np.int32), np.array([0, 30000], dtype=np.int32)
+    size = B.vfm_cattn_fwd_workspace_size(cq, ck, 32, 8, 128)
+    assert size > 0 and size % 256 == 0
+    change = dict(tq=64, cq=cq, tk=30000, ck=ck, H=32, Hk=8, qs=32 * 128, ks=8 * 128, vs=8 * 128)
+    for ws, wsb in ((None, 1 << 40), (0x10000, size - 1), (0x10080, 1 << 40)):
+        assert _fwd(lib, ws=ws, wsb=wsb, **change) == WORKSPACE

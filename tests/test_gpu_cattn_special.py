@@ -47,6 +47,10 @@ CALLS = {
     "many_heads": ((700, 333) * 3, (700, 333) * 3, 32, 8),
     "chunk": ((64, 1), (2900, 700), 8, 2),
     "wide_chunk": ((300, 170), (2000, 170), 12, 4),
+    "a_token_or_two": ((2, 1), (2900, 700), 8, 2),
+    "drafts": ((12, 9), (2500, 100), 8, 2),
+    "long_past": ((1000,), (8000,), 16, 2),
+    "two_long": ((2048, 1900), (2048, 1900), 32, 8),
 }
 
 
@@ -143,7 +147,7 @@ def _expected(host, cq, ck, scale, heads):
 
 
 @pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("name", ["one_sequence", "one_long_to_one", "many", "many_heads", "chunk", "wide_chunk"])
+@pytest.mark.parametrize("name", [n for n in CALLS if n not in ("small", "queries_without_keys", "sixteen_to_one")])
 def test_calls_of_every_cut(name, hd):
     q, kv, heads, kvh = CALLS[name]
     cq, ck, scale = _cu(q), _cu(kv), hd ** -0.5
@@ -159,3 +163,61 @@ def test_calls_of_every_cut(name, hd):
         g = got[x][:, mine] if x in ("out", "dq") else got[x][:, n:n + 1]
         assert U.rel_rms(g, ref[x]) <= tol, (x, U.rel_rms(g, ref[x]))
         U.assert_rows_close(x, g, ref[x], tol, tensor_rms=10 * float(np.sqrt(np.mean(ref[x] * ref[x]))))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_graphs_that_share_a_workspace(hd):
+    """Two captured training steps of different cuts on one workspace, replayed in turn with eager work between, on changing inputs;
+    and the same calls on a stream of the caller's."""
+    import torch
+    b = _binding()
+    scale = hd ** -0.5
+    calls = []
+    for x, name in enumerate(("one_long_to_one", "chunk", "wide_chunk")):
+        q, kv, heads, kvh = CALLS[name]
+        cq, ck = _cu(q), _cu(kv)
+        dev = _inputs(q, kv, heads, kvh, hd, 110 + x)
+        need = [f(cq, ck, heads, kvh, hd) for f in (b.vfm_cattn_fwd_workspace_size, b.vfm_cattn_bwd_workspace_size)]
+        calls.append((dev, cq, ck, need, heads))
+    assert any(c[3][0] for c in calls)                      # (the forward's cut needs one)
+    ws = torch.empty(max(max(c[3]) for c in calls), dtype=torch.uint8, device="cuda")
+
+    def step(c, got):
+        dev, cq, ck = c[:3]
+        b.vfm_cattn_fwd(dev["q"], dev["k"], dev["v"], cq, ck, scale, out=got["out"], lse=got["lse"], workspace=ws)
+        b.vfm_cattn_bwd(dev["q"], dev["k"], dev["v"], got["out"], got["lse"], dev["dout"], cq, ck, scale, got["dq"], got["dk"], got["dv"],
+                        workspace=ws)
+
+    results, graphs = [], []
+    for c in calls:
+        dev = c[0]
+        got = {"out": torch.zeros_like(dev["q"]), "lse": torch.zeros((c[4], dev["q"].shape[0]), device="cuda"), "dq": torch.zeros_like(dev["q"]),
+               "dk": torch.zeros_like(dev["k"]), "dv": torch.zeros_like(dev["v"])}
+        step(c, got)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step(c, got)
+        results.append(got)
+        graphs.append(graph)
+    side = torch.cuda.Stream()
+    for turn in range(3):
+        ws.fill_(255)                                       # (as floats: NaN)
+        wants = [_run(c[0], c[1], c[2], scale) for c in calls]
+        for got in results:
+            for t in got.values():
+                t.zero_()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(results, wants):
+            assert all(torch.equal(got[n], want[n]) for n in want)
+        dev, cq, ck = calls[turn][:3]
+        out, lse = b.vfm_cattn_fwd(dev["q"], dev["k"], dev["v"], cq, ck, scale, stream=side)
+        grads = b.vfm_cattn_bwd(dev["q"], dev["k"], dev["v"], out, lse, dev["dout"], cq, ck, scale, stream=side)
+        side.synchronize()
+        assert all(torch.equal(x, wants[turn][n]) for x, n in zip((out, lse, *grads), ("out", "lse", "dq", "dk", "dv")))
+        for c in calls:
+            for t in c[0].values():
+                t.mul_(0.75)
+        torch.cuda.synchronize()

@@ -396,3 +396,30 @@ def test_sequences_that_share_pages(hd):
     got = b.vfm_kv4_attn(q, *c.bufs, c.pages, _dev_i32(lens), _cu(new), hd ** -0.5, stream=side)
     side.synchronize()
     assert torch.equal(out, got[0]) and torch.equal(lse, got[1])
+
+
+def test_a_cache_past_four_gib():
+    """Pages at the far end of a cache whose codes take 5 GiB a tensor: the same bytes and results as in a small one."""
+    import torch
+    b = _binding()
+    hd, kvh, page, n_pages = 128, 8, 64, 163840
+    lens, new = (150, 63), (2, 1)
+    small = Cache((152, 64), kvh, hd, page, seed=40, spare=0)
+    _fill(small, (152, 64), 41)
+    big = [torch.empty((n_pages, kvh, page, n), dtype=torch.uint8, device="cuda") for n in (64, 64, 4, 4)]
+    assert big[0].numel() == 5 << 30
+    far = Cache((152, 64), kvh, hd, page, seed=40, spare=0)
+    used = int(small.table.max()) + 1
+    far.table = np.where(small.table >= 0, n_pages - used + small.table, -1).astype(np.int32)
+    far.pages.copy_(torch.from_numpy(far.table))
+    far.bufs = big
+    _fill(far, (152, 64), 41)
+    for x, y in zip(b.vfm_kv4_gather(*small.bufs, small.pages, _cu((152, 64))), b.vfm_kv4_gather(*far.bufs, far.pages, _cu((152, 64)))):
+        assert torch.equal(x, y)
+    q = U.to_device(_bits(42, "q", (3, 16, hd)))
+    got = b.vfm_kv4_attn(q, *far.bufs, far.pages, _dev_i32(lens), _cu(new), hd ** -0.5)
+    for t in small.bufs[2:]:
+        t.clamp_(max=254)
+    want = _attend(small, q, lens, _cu(new))
+    # (places of the last pages past the sequences' ends differ: nobody sees them)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
