@@ -6,7 +6,7 @@
 // rows do not all see holds something that is not finite, it forms its sums again: pair by pair from memory, with
 // plain multiplications, over the pairs that are seen.  That is slow, a microsecond or so per key or row, and met only by such inputs.
 // The look itself (an addition per sum) and the code beside the loops cost a call about 1 % (8,000 tokens x 16/1 heads x 128, backward:
-// 860 us without, 868 with; at head_dim 64 nothing measurable but in the cut forward, 4,000 x 8/2: 56.6, 61.5).
+// 860 us without, 868 with).
 #pragma once
 
 #include "cattn_common.h"

@@ -36,6 +36,9 @@ constexpr int kSgcValu = 0x002, kSgcMfma = 0x008, kSgcDsRead = 0x100;
 
 // Wavefronts per SIMD
 constexpr int fwd_waves(int D, int W) { return W == 1 ? 1 : W == 2 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
+// In a cut call, which has a workgroup per CU: room for what the loop over tiles keeps (spilled otherwise: 2,000 tokens x 8/2 heads x 64
+// took 27 us, not 22).
+constexpr int split_waves(int D, int W) { return W == 4 ? (D == 64 ? 2 : 1) : fwd_waves(D, W); }
 
 // A wavefront's sums over keys [j0, j1) hold a NaN: from values that only some of its rows see?
 template <int D>
@@ -429,7 +432,7 @@ __device__ __forceinline__ void split_tile(const SplitPlan& plan, const CausalSh
 }
 
 template <int D, int W>
-__global__ __launch_bounds__(W * 64, fwd_waves(D, W))
+__global__ __launch_bounds__(W * 64, split_waves(D, W))
 void cattn_fwd_split_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
                             __bf16* __restrict__ out, float* __restrict__ lse, const SplitPlan plan, const CausalShape sh,
                             float* __restrict__ slots) {
