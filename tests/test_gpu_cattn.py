@@ -217,3 +217,10 @@ def test_gradients_against_differences():
         got, size = float((U.to_f64(g) * d).sum()), float(np.linalg.norm(U.to_f64(g)))
         # a direction's slope sums the elements' errors with random signs: the norm's bound, four sigma
         assert abs((f[0] - f[1]) / 2e-4 - got) <= 4 * U.TOL_GRAD_RELRMS * size, n
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads", [71, 140])
+def test_groups_wider_than_a_tile(heads, hd):
+    """One K/V head for more query heads than a row block, or a tile, has rows."""
+    _check((9, 1, 70), (40, 1, 70), heads, 1, hd, seed=70 + hd)

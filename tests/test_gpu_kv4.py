@@ -423,3 +423,12 @@ def test_a_cache_past_four_gib():
     want = _attend(small, q, lens, _cu(new))
     # (places of the last pages past the sequences' ends differ: nobody sees them)
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_groups_wider_than_a_row_block(hd):
+    lens, new = (130, 0, 700), (1, 2, 3)
+    have = [a + b for a, b in zip(lens, new)]
+    c = Cache(have, 2, hd, 32, seed=43)
+    _fill(c, have, 44)
+    _attend(c, U.to_device(_bits(45, "q", (sum(new), 140, hd))), lens, _cu(new))
