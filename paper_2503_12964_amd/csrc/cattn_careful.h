@@ -4,7 +4,9 @@
 // such pairs that are multiplied at all lie in the units that cross the diagonal, or next to it in a wavefront's tile.  To look at
 // their operands would cost the loops; so every wavefront looks at its sums once, at the end.  Where they hold a NaN, and what its
 // rows do not all see holds something that is not finite, it forms its sums again: pair by pair from memory, with
-// plain multiplications, over the pairs that are seen.  That is slow, a microsecond or so per key or row, and met only by such inputs.
+// plain multiplications, over the pairs that are seen, until every NaN has been met again.  That is slow, some microseconds per key
+// or row (12,007 tokens x 32/8 heads x 128 with one query of NaNs in the middle: the backward 310 ms, 3.8 without), and lasts only where
+// NaNs did come from what is not seen (with all values NaN in one column: 8.5 ms).
 // The look itself (an addition per sum) and the code beside the loops cost a call about 1 % (8,000 tokens x 16/1 heads x 128, backward:
 // 860 us without, 868 with).
 #pragma once
@@ -37,15 +39,15 @@ __device__ __forceinline__ bool any_nan(const f32x16 (&a)[N]) {   // in any lane
   const float t = (s[0] + s[1]) + (s[2] + s[3]);
   return __builtin_amdgcn_ballot_w64(t != t) != 0;
 }
-template <int N>
-__device__ __forceinline__ bool only_nan(const f32x16 (&a)[N]) {  // in every lane
-  bool all = true;
+// How many of this lane's sums are NaN.  Sums formed again hold none where the first ones do not: as many are the same ones, and then
+// the first ones stand, whatever is still to be added.
+__device__ __forceinline__ int count_nans(const f32x16& a) {
+  int n = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) all &= a[i][e] != a[i][e];
-  return __builtin_amdgcn_ballot_w64(!all) == 0;
+  for (int e = 0; e < 16; ++e) n += a[e] != a[e] ? 1 : 0;
+  return n;
 }
+__device__ __forceinline__ bool as_many_nans(const f32x16& again, int nans) { return __builtin_amdgcn_ballot_w64(count_nans(again) < nans) == 0; }
 __device__ __forceinline__ bool not_finite(u32x4 w) {             // any of eight bf16
   bool bad = false;
 #pragma unroll
@@ -75,24 +77,14 @@ __device__ __forceinline__ float row_dot(const char* a, const char* b) {
   }
   return pair_sum(s);
 }
-// acc += w * row, as the accumulators lie (elements 32 db + 8 q + 4 g + e; row: this lane's first, 4 g)
-template <int D>
-__device__ __forceinline__ void add_row(f32x16 (&acc)[D / 32], float w, const char* row) {
+// acc += w * row, 32 columns as the accumulators lie (elements 8 q + 4 g + e; row: this lane's first, 4 g)
+__device__ __forceinline__ void add_row(f32x16& acc, float w, const char* row) {
 #pragma unroll
-  for (int db = 0; db < D / 32; ++db)
+  for (int q4 = 0; q4 < 4; ++q4) {
+    const bf16x4 x = *reinterpret_cast<const bf16x4*>(row + q4 * 16);
 #pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      const bf16x4 x = *reinterpret_cast<const bf16x4*>(row + db * 64 + q4 * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[db][4 * q4 + e] = __builtin_fmaf(w, (float)x[e], acc[db][4 * q4 + e]);
-    }
-}
-template <int D>
-__device__ __forceinline__ void clear(f32x16 (&acc)[D / 32]) {
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+    for (int e = 0; e < 4; ++e) acc[4 * q4 + e] = __builtin_fmaf(w, (float)x[e], acc[4 * q4 + e]);
+  }
 }
 
 // The first key that not all rows of a wavefront see, at the latest the last key (keys past it are copies of it); wave_min: the last
@@ -102,18 +94,26 @@ __device__ __forceinline__ int first_unseen(int wave_min, int last_key) {
   return j < last_key ? j : last_key;
 }
 
+// The sums are formed again 32 columns at a time: a second set of all of them would not fit beside the first.
+
 // out's sums of 32 rows over keys [j0, j1).  q_row: this lane's; k, v: the sequence's first; lim: last key that the row sees; m: the
 // reference that the sum of its exponentials has.
 template <int D>
 __device__ __forceinline__ void fwd_again(f32x16 (&acc)[D / 32], const char* q_row, const char* k, uint32_t k_row, const char* v,
                                           uint32_t v_row, int j0, int j1, int lim, float m, float scale_log2) {
   const int g = lane_anew() >> 5;
-  clear<D>(acc);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int nans = count_nans(acc[db]);
+    f32x16 sum = {};
+    int j = j0;
 #pragma unroll 1
-  for (int j = j0; j < j1; ++j) {
-    const float s = row_dot<D>(q_row + 16 * g, k + (size_t)j * k_row + 16 * g);
-    if (j <= lim) add_row<D>(acc, fast_exp2(s * scale_log2 - m), v + (size_t)j * v_row + 8 * g);
-    if ((j & 31) == 31 && only_nan(acc)) break;
+    for (; j < j1; ++j) {
+      if ((j & 31) == 0 && as_many_nans(sum, nans)) break;
+      const float s = row_dot<D>(q_row + 16 * g, k + (size_t)j * k_row + 16 * g);
+      if (j <= lim) add_row(sum, fast_exp2(s * scale_log2 - m), v + (size_t)j * v_row + 64 * db + 8 * g);
+    }
+    if (j >= j1) acc[db] = sum;
   }
 }
 
@@ -123,13 +123,19 @@ __device__ __forceinline__ void dq_again(f32x16 (&acc)[D / 32], const char* q_ro
                                          const char* v, uint32_t v_row, int b0, int step, int j1, int lim, float lse2, float delta,
                                          float scale_log2) {
   const int g = lane_anew() >> 5;
-  clear<D>(acc);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int nans = count_nans(acc[db]);
+    f32x16 sum = {};
+    int j = 32 * b0;
 #pragma unroll 1
-  for (int j = 32 * b0; j < j1; j += (j & 31) == 31 ? 32 * step - 31 : 1) {
-    const char* kj = k + (size_t)j * k_row;
-    const float s = row_dot<D>(q_row + 16 * g, kj + 16 * g), dp = row_dot<D>(do_row + 16 * g, v + (size_t)j * v_row + 16 * g);
-    if (j <= lim) add_row<D>(acc, fast_exp2(s * scale_log2 - lse2) * (dp - delta), kj + 8 * g);
-    if ((j & 31) == 31 && only_nan(acc)) break;
+    for (; j < j1; j += (j & 31) == 31 ? 32 * step - 31 : 1) {
+      if ((j & 31) == 0 && as_many_nans(sum, nans)) break;
+      const char* kj = k + (size_t)j * k_row;
+      const float s = row_dot<D>(q_row + 16 * g, kj + 16 * g), dp = row_dot<D>(do_row + 16 * g, v + (size_t)j * v_row + 16 * g);
+      if (j <= lim) add_row(sum, fast_exp2(s * scale_log2 - lse2) * (dp - delta), kj + 64 * db + 8 * g);
+    }
+    if (j >= j1) acc[db] = sum;
   }
 }
 
@@ -140,20 +146,25 @@ __device__ __forceinline__ void dkdv_again(f32x16 (&dk)[D / 32], f32x16 (&dv)[D 
                                            Take take, QAt q_at, DoAt do_at, StatAt stat_at, const float* lse2, const float* delta,
                                            int row_min, float scale_log2) {
   const int g = lane_anew() >> 5;
-  clear<D>(dk);
-  clear<D>(dv);
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db) {
+    const int k_nans = count_nans(dk[db]), v_nans = count_nans(dv[db]);
+    f32x16 sk = {}, sv = {};
+    int r = r1 - 1;
 #pragma unroll 1
-  for (int r = r1 - 1; r >= r0; --r) {
-    if (!take(r >> 5)) { r &= ~31; continue; }
-    const char *qr = q_at(r), *dr = do_at(r);
-    const size_t at = stat_at(r);
-    const float s = row_dot<D>(qr + 16 * g, k_row + 16 * g), dp = row_dot<D>(dr + 16 * g, v_row + 16 * g);
-    if (r >= row_min) {
-      const float p = fast_exp2(s * scale_log2 - lse2[at]);
-      add_row<D>(dk, p * (dp - delta[at]), qr + 8 * g);
-      add_row<D>(dv, p, dr + 8 * g);
+    for (; r >= r0; --r) {
+      if (!take(r >> 5)) { r &= ~31; continue; }
+      if ((r & 31) == 31 && as_many_nans(sk, k_nans) && as_many_nans(sv, v_nans)) break;
+      const char *qr = q_at(r), *dr = do_at(r);
+      const size_t at = stat_at(r);
+      const float s = row_dot<D>(qr + 16 * g, k_row + 16 * g), dp = row_dot<D>(dr + 16 * g, v_row + 16 * g);
+      if (r >= row_min) {
+        const float p = fast_exp2(s * scale_log2 - lse2[at]);
+        add_row(sk, p * (dp - delta[at]), qr + 64 * db + 8 * g);
+        add_row(sv, p, dr + 64 * db + 8 * g);
+      }
     }
-    if ((r & 31) == 0 && only_nan(dk) && only_nan(dv)) break;
+    if (r < r0) { dk[db] = sk; dv[db] = sv; }
   }
 }
 

@@ -459,10 +459,13 @@ void cattn_dq2_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
 #pragma unroll
   for (int ib = 0; ib < 2; ++ib) wait_mfma_a(dqacc[ib][0], dqacc[ib][1], dqacc[ib][2], dqacc[ib][3]);
 
-#pragma unroll
-  for (int ib = 0; ib < 2; ++ib)
-    if (any_nan(dqacc[ib]))   // (rare)
+  auto checked = [&](auto ib_c) {       // (rare)
+    constexpr int ib = decltype(ib_c)::value;
+    if (any_nan(dqacc[ib]))
       dq_checked<D>(dqacc[ib], q, k, v, dout, cs, shape_anew(sh), kvh, row_w + ib * 32, 0, 1, wave_tiles * kCDqBC, true, lse2[ib], dlt[ib]);
+  };
+  checked(IntC<0>{});
+  checked(IntC<1>{});
 
   // ---- epilogue: dq = bf16(scale * dQ^T), whole rows per store
   __syncthreads();   // the ring is free: each wavefront turns its tiles through a piece of it

@@ -221,3 +221,21 @@ def test_graphs_that_share_a_workspace(hd):
             for t in c[0].values():
                 t.mul_(0.75)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("where", ["v", "dout"])
+def test_one_column_not_finite(where, hd):
+    """One element of every value, or of every row of dout: out's (dv's) other columns are as without."""
+    q, kv, heads, kvh = CALLS["one_long_to_one"]
+    cq, ck, scale = _cu(q), _cu(kv), hd ** -0.5
+    dev = _inputs(q, kv, heads, kvh, hd, 120 + hd)
+    clean = _run(dev, cq, ck, scale)
+    dev[where][..., 37] = float("nan")
+    got = _run(dev, cq, ck, scale)
+    bad = {n: np.zeros(tuple(t.shape), dtype=bool) for n, t in clean.items()}
+    bad["dq"][:] = bad["dk"][:] = True
+    bad["out" if where == "v" else "dv"][..., 37] = True
+    for n, tol in (("out", U.TOL_OUT_RELRMS), ("lse", U.TOL_LSE_MAXABS), ("dq", U.TOL_GRAD_RELRMS), ("dk", U.TOL_GRAD_RELRMS),
+                   ("dv", U.TOL_GRAD_RELRMS)):
+        _compare(n, got[n], clean[n], bad[n], tol)
