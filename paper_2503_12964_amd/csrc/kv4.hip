@@ -4,6 +4,8 @@
 // head_dim / 8 lanes share a row, 8 elements (16 bytes of bf16, 4 bytes of codes) a lane, so that a wavefront's
 // loads and stores are whole rows on both sides; the four lanes of a block find its maximum by two lane
 // exchanges.  A workgroup takes consecutive rows (token-major, head-minor) of K and of V.
+// Measured, 8 K/V heads x 128: 12,087 tokens written in 16 us (63 MB, 3.9 TB/s), 23,809 read back in 27 us (123 MB, 4.5 TB/s; a large
+// copy reaches 4.6).  Requesting a row before its place is looked up: 18 us.
 #include "kv4_common.h"
 
 namespace vfm {
