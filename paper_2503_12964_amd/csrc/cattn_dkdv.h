@@ -193,8 +193,9 @@ void cattn_dkdv_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ 
   // ---- tile requests (direct global->LDS).  Lane L of wave instruction (x, wave) owns LDS chunk (x*waves + wave)*64 + L:
   // row P / chunks_per_row, physical chunk P % chunks_per_row (the swizzle has a period of 16 rows, so the logical chunk
   // does not depend on x).  Offsets count from the sequence's first query and step back by a tile; past the last row
-  // they clamp to it, and so do those that the requests ahead of the walk's end bring below row 0 (wrapped, they are large).  Waves 0/2 fetch lse2, waves 1/3 Delta: 0 and 1 of a tile's first 64 rows, 2 and 3 of the others (of the
-  // same into spare LDS where there are none).
+  // they clamp to it, and so do those that the requests ahead of the walk's end bring below row 0 (wrapped, they are large).
+  // Waves 0/2 fetch lse2, waves 1/3 Delta: 0 and 1 of a tile's first 64 rows, 2 and 3 of the others (of the same into spare LDS
+  // where there are none).
   const uint32_t do_row = (uint32_t)sh.n_heads * RB;
   const int d_tok = kBQ / sh.group, d_sub = kBQ - d_tok * sh.group;
   const uint32_t q_step = (uint32_t)d_tok * sh.q_row + (uint32_t)d_sub * RB, q_wrap = sh.q_row - (uint32_t)sh.group * RB;

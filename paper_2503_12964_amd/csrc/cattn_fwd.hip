@@ -470,7 +470,8 @@ void cattn_fwd_join_kernel(__bf16* __restrict__ out, float* __restrict__ lse, co
   split_tile(plan, sh, W * 32, tile, seq, tq, units);
   const CausalSeq cs = causal_seq(plan, seq, sh.group);
   __shared__ __attribute__((aligned(16))) float shares[(kJoinShares - 1) * (D / 32)][18][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), db = wave % (D / 32), share = wave / (D / 32), lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), db = wave % (D / 32), share = wave / (D / 32);
+  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
   const int row_w = tq * W * 32 + blockIdx.y * 32;
   if (row_w >= cs.rows) return;
   // the tile's parts: pieces p - 1 .. last (empty pieces among them have none)
