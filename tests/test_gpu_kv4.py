@@ -432,3 +432,21 @@ def test_groups_wider_than_a_row_block(hd):
     c = Cache(have, 2, hd, 32, seed=43)
     _fill(c, have, 44)
     _attend(c, U.to_device(_bits(45, "q", (sum(new), 140, hd))), lens, _cu(new))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_a_cache_without_pages(hd):
+    import torch
+    pkg = _binding()
+    # no memory at all behind the table's entries: nothing is written, zeros are read, no token sees anything
+    kvh, heads, page, cu = 2, 8, 16, np.array([0, 1, 6], np.int32)
+    cache = [torch.empty((0, kvh, page, n), dtype=torch.uint8, device="cuda") for n in (hd // 2, hd // 2, hd // 32, hd // 32)]
+    pages = torch.zeros((2, 40), dtype=torch.int32, device="cuda")
+    lens = torch.tensor([600, 3], dtype=torch.int32, device="cuda")
+    kv = torch.ones((6, kvh, hd), dtype=torch.bfloat16, device="cuda")
+    q = torch.ones((6, heads, hd), dtype=torch.bfloat16, device="cuda")
+    pkg.vfm_kv4_append(kv, kv, *cache, pages, lens, cu)
+    k, v = pkg.vfm_kv4_gather(*cache, pages, cu, torch.ones_like(kv), torch.ones_like(kv))
+    assert not k.any() and not v.any()
+    out, lse = pkg.vfm_kv4_attn(q, *cache, pages, lens, cu, hd ** -0.5, torch.ones_like(q))
+    assert not out.any() and bool((lse == -float("inf")).all())
