@@ -189,8 +189,8 @@ void cattn_dq_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k,
     }
     wait_vmcnt<0>();
     __syncthreads();
-    if (any_nan(dqacc))       // (rare; values that are not seen take no part: see the mask)
-      dq_checked<D>(dqacc, q, k, v, dout, cs, shape_anew(sh), kvh, row_w, kg, KG, n_tiles * Cfg::kBC, false, lse2, dlt);
+    if (any_nan(dqacc))       // (rare)
+      dq_checked<D>(dqacc, q, k, v, dout, cs, shape_anew(sh), kvh, row_w, kg, KG, n_tiles * Cfg::kBC, lse2, dlt);
   }
   if constexpr (KG > 1) {
     auto sums = [&](int x) { return reinterpret_cast<f32x4*>(smem + Cfg::kTurn) + (size_t)((x - 1) * (4 / KG) + rw) * (8 * D); };

@@ -1,12 +1,13 @@
 // Keys and rows that hold a NaN or an infinity, for those that do not see them.  Included by the causal attention kernels.
 //
 // A pair (row, key) that is not seen has weight 0 in the second products, but 0 times a NaN or an infinity is a NaN.  The only
-// such pairs that are multiplied at all lie in the units that cross the diagonal, or next to it in a wavefront's tile.  To look at
-// their operands would cost the loops; so every wavefront looks at its sums once, at the end.  Where they hold a NaN, and what its
-// rows do not all see holds something that is not finite, it forms its sums again: pair by pair from memory, with
+// such pairs that are multiplied at all lie in the units that cross the diagonal, or next to it in a wavefront's tile, and among the
+// copies of the last row or key that fill a last tile.  Where it comes from is not asked: besides the operands themselves it may be a
+// product of finite ones that overflows (dP or Delta).  To look at the pairs would cost the loops; so every wavefront looks at its
+// sums once, at the end.  Where they hold a NaN it forms them again: pair by pair from memory, with
 // plain multiplications, over the pairs that are seen, until every NaN has been met again.  That is slow, some microseconds per key
-// or row (12,007 tokens x 32/8 heads x 128 with one query of NaNs in the middle: the backward 310 ms, 3.8 without), and lasts only where
-// NaNs did come from what is not seen (with all values NaN in one column: 8.5 ms).
+// or row (12,007 tokens x 32/8 heads x 128 with one query of NaNs in the middle: the backward 674 ms, 3.8 without), and lasts only where
+// NaNs did come from what is not seen (with all values NaN in one column: 8.1 ms).
 // The look itself (an addition per sum) and the code beside the loops cost a call about 1 % (8,000 tokens x 16/1 heads x 128, backward:
 // 860 us without, 868 with).
 #pragma once
@@ -48,23 +49,6 @@ __device__ __forceinline__ int count_nans(const f32x16& a) {
   return n;
 }
 __device__ __forceinline__ bool as_many_nans(const f32x16& again, int nans) { return __builtin_amdgcn_ballot_w64(count_nans(again) < nans) == 0; }
-__device__ __forceinline__ bool not_finite(u32x4 w) {             // any of eight bf16
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) bad |= (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return bad;
-}
-// Whether rows [r0, r1) hold anything that is not finite; at(r): address of row r.  The whole wavefront asks.
-template <int D, class At>
-__device__ __forceinline__ bool rows_not_finite(int r0, int r1, At at) {
-  constexpr int CPR = D / 8;
-  const int lane = lane_anew();
-  bool bad = false;
-#pragma unroll 1
-  for (int r = r0 + lane / CPR; r < r1; r += 64 / CPR)
-    bad |= not_finite(*reinterpret_cast<const u32x4*>(at(r) + lane % CPR * 16));
-  return __builtin_amdgcn_ballot_w64(bad) != 0;
-}
 // This lane's half (elements 16 ks + 8 g + e) of the product of two rows, summed with the other half's
 template <int D>
 __device__ __forceinline__ float row_dot(const char* a, const char* b) {
@@ -85,13 +69,6 @@ __device__ __forceinline__ void add_row(f32x16& acc, float w, const char* row) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[4 * q4 + e] = __builtin_fmaf(w, (float)x[e], acc[4 * q4 + e]);
   }
-}
-
-// The first key that not all rows of a wavefront see, at the latest the last key (keys past it are copies of it); wave_min: the last
-// that its first row sees.
-__device__ __forceinline__ int first_unseen(int wave_min, int last_key) {
-  const int j = wave_min < 0 ? 0 : wave_min + 1;
-  return j < last_key ? j : last_key;
 }
 
 // The sums are formed again 32 columns at a time: a second set of all of them would not fit beside the first.

@@ -86,7 +86,7 @@ __device__ __forceinline__ KvWalk kv_walk(int block, const XSegTable& segs, cons
   return w;
 }
 
-// A wavefront's sums hold a NaN: from rows that only some of its keys are seen by?
+// A wavefront's sums hold a NaN: they are formed again over the rows that see each key.
 template <int D, int RG>
 __device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32], int wave, const __bf16* q, const __bf16* k,
                                              const __bf16* v, const __bf16* dout, const float* lse2, const float* delta,
@@ -96,7 +96,7 @@ __device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[
   const CausalSeq& cs = w.cs;
   const int rg = wave / (kCBwdWaves / RG), jw = w.j0 + wave % (kCBwdWaves / RG) * 32;
   const int row0 = first_row_of(cs, sh.group, jw), r_first = row0 <= w.rt0 ? w.rt0 : row0 / kBQ * kBQ;
-  const int r_end = min(w.rt0 + w.n_tiles * kBQ, cs.rows), r_some = min(first_row_of(cs, sh.group, jw + 31), r_end);
+  const int r_end = min(w.rt0 + w.n_tiles * kBQ, cs.rows);
   auto row_at = [&](const __bf16* base, size_t row_bytes, int r) {
     const int tok = r / sh.group;
     return (const char*)base + (size_t)(cs.qs + tok) * row_bytes + (size_t)(w.kvh * sh.group + r - tok * sh.group) * RB;
@@ -107,17 +107,6 @@ __device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[
     const int tok = r / sh.group;
     return (size_t)(w.kvh * sh.group + r - tok * sh.group) * sh.total_q + cs.qs + tok;
   };
-  bool bad = rows_not_finite<D>(r_first, r_some, q_at) || rows_not_finite<D>(r_first, r_some, do_at);
-  if (!bad) {
-    bool nan = false;
-#pragma unroll 1
-    for (int r = r_first + lane_anew(); r < r_some; r += 64) {
-      const float a = lse2[stat_at(r)], b = delta[stat_at(r)];
-      nan |= a != a || b != b;
-    }
-    bad = __builtin_amdgcn_ballot_w64(nan) != 0;
-  }
-  if (!bad) return;
   const int key = min(jw + (lane_anew() & 31), cs.kl - 1);
   dkdv_again<D>(dk, dv, (const char*)k + (size_t)(cs.ks + key) * sh.k_row + (size_t)w.kvh * RB,
                 (const char*)v + (size_t)(cs.ks + key) * sh.v_row + (size_t)w.kvh * RB, r_first, r_end,

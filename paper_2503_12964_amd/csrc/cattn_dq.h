@@ -50,20 +50,16 @@ __device__ __forceinline__ float row16_total(float v) {
   return v;
 }
 
-// The sums of a wavefront's 32 rows over the 32-key blocks b0, b0 + step .. below key j1 hold a NaN: from keys (or values, if those
-// take part) that only some of the rows see, or from a row that sees none?
+// The sums of a wavefront's 32 rows over the 32-key blocks b0, b0 + step .. below key j1 hold a NaN: they are formed again over the
+// keys that each row sees.
 template <int D>
 __device__ __forceinline__ void dq_checked(f32x16 (&acc)[D / 32], const __bf16* q, const __bf16* k, const __bf16* v, const __bf16* dout,
                                            const CausalSeq& cs, const CausalShape& sh, int kvh, int row_w, int b0, int step, int j1,
-                                           bool values, float lse2, float delta) {
+                                           float lse2, float delta) {
   constexpr int RB = D * 2;
   const char* kbase = (const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB;
   const char* vbase = (const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB;
   j1 = min(j1, cs.kl);
-  const int first = min(row_w, cs.rows - 1) / sh.group + cs.off, j0 = first_unseen(first, cs.kl - 1);
-  if (first >= 0 && !rows_not_finite<D>(j0, j1, [&](int j) { return kbase + (size_t)j * sh.k_row; }) &&
-      !(values && rows_not_finite<D>(j0, j1, [&](int j) { return vbase + (size_t)j * sh.v_row; })))
-    return;
   const int row = min(row_w + (lane_anew() & 31), cs.rows - 1), tok = row / sh.group, head = kvh * sh.group + row - tok * sh.group;
   dq_again<D>(acc, (const char*)q + (size_t)(cs.qs + tok) * sh.q_row + (size_t)head * RB,
               (const char*)(dout + ((size_t)(cs.qs + tok) * sh.n_heads + head) * D), kbase, sh.k_row, vbase, sh.v_row, b0, step, j1,
@@ -463,7 +459,7 @@ void cattn_dq2_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
   auto checked = [&](auto ib_c) {       // (rare)
     constexpr int ib = decltype(ib_c)::value;
     if (any_nan(dqacc[ib]))
-      dq_checked<D>(dqacc[ib], q, k, v, dout, cs, shape_anew(sh), kvh, row_w + ib * 32, 0, 1, wave_tiles * kCDqBC, true, lse2[ib], dlt[ib]);
+      dq_checked<D>(dqacc[ib], q, k, v, dout, cs, shape_anew(sh), kvh, row_w + ib * 32, 0, 1, wave_tiles * kCDqBC, lse2[ib], dlt[ib]);
   };
   checked(IntC<0>{});
   checked(IntC<1>{});
