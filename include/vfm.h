@@ -424,8 +424,9 @@ VFM_API int vfm_attn_fwd_tile_rows(const int32_t* cu_seqlens, int n_seqs, int to
  * total_q * n_heads <= 2^27 and total_kv * n_kv_heads <= 2^28 (SHAPE).  k and v may be
  * NULL if total_kv is 0.  out and lse must not overlap the inputs.
  * What a query or a key does not see has no part in its results, not even a NaN or an
- * infinity there (but many of them cost time).  The result is bitwise reproducible from
- * run to run; how a call is cut into pieces depends on all of its sizes and on the
+ * infinity there, or a product that overflows.  Where sums have met such values they are
+ * formed again more slowly: the call may take up to about ten times as long.
+ * The result is bitwise reproducible from run to run; how a call is cut into pieces depends on all of its sizes and on the
  * number of compute units, and with it the order in which the fp32 sums are formed.
  * workspace: device, 256-byte aligned, vfm_cattn_fwd_workspace_size() bytes for the
  * current device (0: none needed, may be NULL); its contents need not be initialised.

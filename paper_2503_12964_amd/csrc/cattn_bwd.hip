@@ -37,7 +37,7 @@ struct CDqCfg {
   static_assert(kTurn + (KG - 1) * (4 / KG) * 32 * D * 4 <= kLdsBytes, "the others' sums");
   static constexpr int kChunksPerRow = D / 8;
   static constexpr int kLoadsPerWave = kBC * kChunksPerRow / 256;
-  static constexpr int kWaves = D == 64 ? (KG == 1 ? 3 : KG == 2 ? 2 : 1) : 1;   // per SIMD
+  static constexpr int kWaves = D == 64 ? (KG == 4 ? 1 : 3) : 1;   // per SIMD
 };
 
 template <int D, int KG>

@@ -86,7 +86,7 @@ __device__ __forceinline__ KvWalk kv_walk(int block, const XSegTable& segs, cons
   return w;
 }
 
-// A wavefront's sums hold a NaN: they are formed again over the rows that see each key.
+// A wavefront's sums hold a NaN: they are formed again over the rows that see each key, if those that do not may have made one.
 template <int D, int RG>
 __device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32], int wave, const __bf16* q, const __bf16* k,
                                              const __bf16* v, const __bf16* dout, const float* lse2, const float* delta,
@@ -97,21 +97,18 @@ __device__ __forceinline__ void dkdv_checked(f32x16 (&dk)[D / 32], f32x16 (&dv)[
   const int rg = wave / (kCBwdWaves / RG), jw = w.j0 + wave % (kCBwdWaves / RG) * 32;
   const int row0 = first_row_of(cs, sh.group, jw), r_first = row0 <= w.rt0 ? w.rt0 : row0 / kBQ * kBQ;
   const int r_end = min(w.rt0 + w.n_tiles * kBQ, cs.rows);
-  auto row_at = [&](const __bf16* base, size_t row_bytes, int r) {
-    const int tok = r / sh.group;
-    return (const char*)base + (size_t)(cs.qs + tok) * row_bytes + (size_t)(w.kvh * sh.group + r - tok * sh.group) * RB;
-  };
-  auto q_at = [&](int r) { return row_at(q, sh.q_row, r); };
-  auto do_at = [&](int r) { return row_at(dout, (size_t)sh.n_heads * RB, r); };
-  auto stat_at = [&](int r) {
-    const int tok = r / sh.group;
-    return (size_t)(w.kvh * sh.group + r - tok * sh.group) * sh.total_q + cs.qs + tok;
+  auto at = [&](int r) -> RowAt {
+    const int tok = r / sh.group, sub = r - tok * sh.group;
+    return {(uint32_t)tok * sh.q_row + (uint32_t)sub * RB, ((uint32_t)tok * sh.n_heads + sub) * RB,
+            (size_t)(w.kvh * sh.group + sub) * sh.total_q + cs.qs + tok};
   };
   const int key = min(jw + (lane_anew() & 31), cs.kl - 1);
   dkdv_again<D>(dk, dv, (const char*)k + (size_t)(cs.ks + key) * sh.k_row + (size_t)w.kvh * RB,
                 (const char*)v + (size_t)(cs.ks + key) * sh.v_row + (size_t)w.kvh * RB, r_first, r_end,
-                [&](int block) { return RG == 1 || block % RG == rg; }, q_at, do_at, stat_at, lse2, delta,
-                first_row_of(cs, sh.group, key), sh.scale_log2);
+                w.rt0 + w.n_tiles * kBQ, [&](int block) { return RG == 1 || block % RG == rg; },
+                (const char*)q + (size_t)cs.qs * sh.q_row + (size_t)w.kvh * sh.group * RB,
+                (const char*)dout + ((size_t)cs.qs * sh.n_heads + (size_t)w.kvh * sh.group) * RB, at, lse2, delta,
+                first_row_of(cs, sh.group, key), first_row_of(cs, sh.group, jw + 31), sh.scale_log2);
 }
 
 template <int D, int RG>

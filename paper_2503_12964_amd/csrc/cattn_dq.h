@@ -51,7 +51,7 @@ __device__ __forceinline__ float row16_total(float v) {
 }
 
 // The sums of a wavefront's 32 rows over the 32-key blocks b0, b0 + step .. below key j1 hold a NaN: they are formed again over the
-// keys that each row sees.
+// keys that each row sees, if those that it does not see may have made one.
 template <int D>
 __device__ __forceinline__ void dq_checked(f32x16 (&acc)[D / 32], const __bf16* q, const __bf16* k, const __bf16* v, const __bf16* dout,
                                            const CausalSeq& cs, const CausalShape& sh, int kvh, int row_w, int b0, int step, int j1,
@@ -59,11 +59,11 @@ __device__ __forceinline__ void dq_checked(f32x16 (&acc)[D / 32], const __bf16* 
   constexpr int RB = D * 2;
   const char* kbase = (const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB;
   const char* vbase = (const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB;
-  j1 = min(j1, cs.kl);
   const int row = min(row_w + (lane_anew() & 31), cs.rows - 1), tok = row / sh.group, head = kvh * sh.group + row - tok * sh.group;
   dq_again<D>(acc, (const char*)q + (size_t)(cs.qs + tok) * sh.q_row + (size_t)head * RB,
-              (const char*)(dout + ((size_t)(cs.qs + tok) * sh.n_heads + head) * D), kbase, sh.k_row, vbase, sh.v_row, b0, step, j1,
-              tok + cs.off, lse2, delta, sh.scale_log2);
+              (const char*)(dout + ((size_t)(cs.qs + tok) * sh.n_heads + head) * D), kbase, sh.k_row, vbase, sh.v_row, b0, step,
+              (min(row_w + 32, cs.rows) - 1) / sh.group + cs.off + 1, j1, cs.kl - 1, tok + cs.off,
+              min(row_w, cs.rows - 1) / sh.group + cs.off, lse2, delta, sh.scale_log2);
 }
 
 template <int D>

@@ -42,17 +42,18 @@ constexpr int fwd_waves(int D, int W) { return W == 1 ? 1 : W == 2 ? (D == 64 ? 
 // took 27 us, not 22).
 constexpr int split_waves(int D, int W) { return W == 4 ? (D == 64 ? 2 : 1) : fwd_waves(D, W); }
 
-// A wavefront's sums over keys [j0, j1) hold a NaN: they are formed again over the keys that each row sees.
+// A wavefront's sums over keys [j0, j1) hold a NaN: they are formed again over the keys that each row sees, if those that
+// it does not see may have made one.
 template <int D>
 __device__ __forceinline__ void fwd_checked(f32x16 (&acc)[D / 32], const __bf16* q, const __bf16* k, const __bf16* v,
                                             const CausalSeq& cs, const CausalShape& sh, int kvh, int row_w, int j0, int j1, float m) {
   constexpr int RB = D * 2;
   const char* kbase = (const char*)k + (size_t)cs.ks * sh.k_row + (size_t)kvh * RB;
   const char* vbase = (const char*)v + (size_t)cs.ks * sh.v_row + (size_t)kvh * RB;
-  j1 = min(j1, cs.kl);
   const int row = min(row_w + (lane_anew() & 31), cs.rows - 1), tok = row / sh.group;
   const char* q_row = (const char*)q + (size_t)(cs.qs + tok) * sh.q_row + (size_t)(kvh * sh.group + row - tok * sh.group) * RB;
-  fwd_again<D>(acc, q_row, kbase, sh.k_row, vbase, sh.v_row, j0, j1, tok + cs.off, m, sh.scale_log2);
+  fwd_again<D>(acc, q_row, kbase, sh.k_row, vbase, sh.v_row, j0, min(j1, cs.kl), j1, tok + cs.off, min(row_w, cs.rows - 1) / sh.group + cs.off, m,
+               sh.scale_log2);
 }
 
 // What a workgroup does of one tile: the units [u0, u1) of the keys that the tile's last row sees.  slot: null, or where the

@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from tests import parity_utils as U
-from tests.test_gpu_cattn_special import CALLS, _cu, _inputs, _run
+from tests.test_gpu_cattn_special import CALLS, _binding, _cu, _inputs, _run
 
 pytestmark = pytest.mark.gpu
 
@@ -141,3 +141,37 @@ def test_products_of_unseen_pairs_may_overflow(name, hd):
     _same_rows("dq", got["dq"], small_v["dq"], rows)
     _same_rows("dk", got["dk"], small_dout["dk"], keys)
     _same_rows("dv", got["dv"], small_dout["dv"], keys)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("what", ["a query of NaN", "a column of infinities"])
+def test_the_backward_stays_within_a_few_times_its_time(what, hd):
+    """Sums that are formed again take their blocks straight from memory, without the loops' pipeline: some ten times the time of a
+    block, for the wavefronts that met such values or for all of them.  25 leaves room for the clock; one pair at a time it
+    was 50 to 80 times here, and more the longer the sequence."""
+    import time
+    import torch
+    b = _binding()
+    n, heads, kvh = 10000, 16, 4
+    cu, scale = _cu((n,)), hd ** -0.5
+    dev = _inputs((n,), (n,), heads, kvh, hd, 180 + hd)
+
+    def best():
+        out, lse = b.vfm_cattn_fwd(dev["q"], dev["k"], dev["v"], cu, cu, scale)
+        times = []
+        for _ in range(4):
+            torch.cuda.synchronize()
+            t = time.perf_counter()
+            b.vfm_cattn_bwd(dev["q"], dev["k"], dev["v"], out, lse, dev["dout"], cu, cu, scale)
+            torch.cuda.synchronize()
+            times.append(time.perf_counter() - t)
+        return min(times)
+
+    clean = best()
+    if what == "a query of NaN":
+        dev["q"][n // 2, 3] = float("nan")
+    else:
+        dev["dout"][..., 5] = float("inf")
+    taken = best()
+    print(f"{what}, head_dim {hd}: {clean * 1e3:.2f} ms, {taken * 1e3:.2f} with it")
+    assert taken <= 25 * clean
