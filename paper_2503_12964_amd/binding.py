@@ -525,10 +525,15 @@ def _workspace(given, size, sizes, like, here: int, stream):
     return given, given.data_ptr(), given.numel() * given.element_size()
 
 
-def _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv):
+def _causal_cu(cu_seqlens_q, cu_seqlens_kv):
     cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
     if cq.size != ck.size or cq.size < 1:
         raise ValueError("cu_seqlens_q and cu_seqlens_kv must have the same length")
+    return cq, ck
+
+
+def _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv):
+    cq, ck = _causal_cu(cu_seqlens_q, cu_seqlens_kv)
     sq, sk = q.shape, k.shape
     if len(sq) != 3 or len(sk) != 3 or sk[2] != sq[2]:
         raise ValueError("q [total_q, heads, head_dim], k and v [total_kv, kv_heads, head_dim] expected")
@@ -538,7 +543,7 @@ def _causal_sizes(q, k, cu_seqlens_q, cu_seqlens_kv):
 
 def vfm_cattn_fwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
     lib = _calls or load_library().by_address
-    cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
+    cq, ck = _causal_cu(cu_seqlens_q, cu_seqlens_kv)
     return int(lib.vfm_cattn_fwd_workspace_size(_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, int(cq[-1]), int(ck[-1]), int(n_heads),
                                                 int(n_kv_heads), int(head_dim)))
 
@@ -559,7 +564,7 @@ def vfm_cattn_fwd(q, k, v, cu_seqlens_q, cu_seqlens_kv, scale: float, out=None, 
 
 def vfm_cattn_bwd_workspace_size(cu_seqlens_q, cu_seqlens_kv, n_heads: int, n_kv_heads: int, head_dim: int) -> int:
     lib = _calls or load_library().by_address
-    cq, ck = _host_i32(cu_seqlens_q), _host_i32(cu_seqlens_kv)
+    cq, ck = _causal_cu(cu_seqlens_q, cu_seqlens_kv)
     return int(lib.vfm_cattn_bwd_workspace_size(_i32_ptr(cq), _i32_ptr(ck), cq.size - 1, int(cq[-1]), int(ck[-1]), int(n_heads),
                                                 int(n_kv_heads), int(head_dim)))
 
