@@ -485,16 +485,21 @@ def _like(t, name: str, here: int, shape, dtype) -> int:
     return t.data_ptr()
 
 
-def _new(shape, dtype, like, stream):
-    """A tensor for the kernels of this call.  It belongs to the current stream; if they run on another, tell the allocator."""
-    if like.dtype is dtype and like.shape == shape and like.is_contiguous():
-        t = _torch.empty_like(like)          # (a third less than the general call)
-    else:
-        t = _torch.empty(shape, dtype=dtype, device=like.device)
-    if stream is not None and t.numel():
+def _new(shape, dtype, like, stream, result=True):
+    """A tensor for the kernels of this call, from the memory of the stream that they run on: what the current stream has freed may
+    still be in use by work in front of it.  A result lives on until the current stream, where the caller goes on, is done with it too."""
+    here = s = None
+    if stream is not None:
+        here = _torch.cuda.current_stream()
         s = stream if hasattr(stream, "cuda_stream") else _torch.cuda.ExternalStream(int(stream))
-        if s.cuda_stream != _torch.cuda.current_stream().cuda_stream:
-            t.record_stream(s)
+    if s is None or s.cuda_stream == here.cuda_stream:
+        if like.dtype is dtype and like.shape == shape and like.is_contiguous():
+            return _torch.empty_like(like)          # (a third less than the general call)
+        return _torch.empty(shape, dtype=dtype, device=like.device)
+    with _torch.cuda.stream(s):
+        t = _torch.empty(shape, dtype=dtype, device=like.device)
+    if result and t.numel():
+        t.record_stream(here)
     return t
 
 
@@ -518,7 +523,7 @@ def _workspace(given, size, sizes, like, here: int, stream):
         need = size(*sizes)
         if not need:
             return None, 0, 0
-        given = _new(need, _torch.uint8, like, stream)
+        given = _new(need, _torch.uint8, like, stream, result=False)
         return given, given.data_ptr(), need
     if given.get_device() != here or not given.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor of the current device")

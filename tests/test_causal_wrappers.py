@@ -22,3 +22,43 @@ def test_workspace_sizes_ask_for_as_many_boundaries_of_keys_as_of_queries(size, 
     """The library reads n_seqs + 1 of either: a shorter array would be read past its end."""
     with pytest.raises(ValueError):
         size(cq, ck, 4, 2, 128)
+
+
+class _Streams:
+    """As much of torch as the wrappers allocate with: notes the stream that every tensor is asked for on, and whose end it outlives."""
+
+    def __init__(self):
+        import contextlib
+        import types
+        self.now, self.made, self.uint8, outer = types.SimpleNamespace(cuda_stream=7), [], "uint8", self
+
+        @contextlib.contextmanager
+        def stream(s):
+            was, outer.now = outer.now, s
+            yield
+            outer.now = was
+
+        def empty(shape, dtype=None, device=None):
+            t = types.SimpleNamespace(numel=lambda: 1, data_ptr=lambda: 0, on=outer.now.cuda_stream, kept_for=[])
+            t.record_stream = lambda s: t.kept_for.append(s.cuda_stream)
+            outer.made.append(t)
+            return t
+
+        self.empty, self.empty_like = empty, lambda like: empty(None)
+        self.cuda = types.SimpleNamespace(current_stream=lambda: outer.now, stream=stream,
+                                          ExternalStream=lambda x: types.SimpleNamespace(cuda_stream=x))
+
+
+@pytest.mark.parametrize("stream,on,kept_for", [(None, 7, []), (7, 7, []), (9, 9, [7])])
+def test_tensors_come_from_the_memory_of_the_stream_that_the_kernels_run_on(monkeypatch, stream, on, kept_for):
+    """The current stream's allocator may hand out what work in front of that stream still uses; another stream would not wait for it."""
+    import types
+    import torch
+    fake = _Streams()
+    monkeypatch.setattr(B, "_torch", fake)
+    like = types.SimpleNamespace(dtype=torch.bfloat16, shape=(3, 2, 64), device="cuda", is_contiguous=lambda: True)
+    for shape in ((3, 2, 64), (5, 2, 64)):
+        B._new(shape, torch.bfloat16, like, stream)
+    B._workspace(None, lambda: 100, (), like, 0, stream)
+    assert [t.on for t in fake.made] == [on] * 3
+    assert [t.kept_for for t in fake.made] == [kept_for, kept_for, []]
