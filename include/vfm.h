@@ -420,9 +420,10 @@ VFM_API int vfm_attn_fwd_tile_rows(const int32_t* cu_seqlens, int n_seqs, int to
  * 8; the heads of a token are contiguous), so that they may be parts of one
  * projection's output; out: bf16 [total_q, n_heads, head_dim] and lse: fp32
  * [n_heads, total_q], contiguous, fully overwritten.  Both cu arrays are host
- * int32 [n_seqs+1].  One sequence's rows of a tensor span less than 4 GiB,
- * total_q * n_heads <= 2^27 and total_kv * n_kv_heads <= 2^28 (SHAPE).  k and v may be
- * NULL if total_kv is 0.  out and lse must not overlap the inputs.
+ * int32 [n_seqs+1].  The longest sequence's rows of q, k or v and 512 more, which
+ * requests ahead may count up to, span less than 4 GiB ((tokens + 512) * stride * 2 bytes,
+ * whatever the length), total_q * n_heads <= 2^27 and total_kv * n_kv_heads <= 2^28 (SHAPE).
+ * k and v may be NULL if total_kv is 0.  out and lse must not overlap the inputs.
  * What a query or a key does not see has no part in its results, not even a NaN or an
  * infinity there, or a product that overflows.  Where sums have met such values they are
  * formed again more slowly: the call may take up to about ten times as long.

@@ -62,3 +62,19 @@ def test_tensors_come_from_the_memory_of_the_stream_that_the_kernels_run_on(monk
     B._workspace(None, lambda: 100, (), like, 0, stream)
     assert [t.on for t in fake.made] == [on] * 3
     assert [t.kept_for for t in fake.made] == [kept_for, kept_for, []]
+
+
+@pytest.mark.parametrize("tokens", [1, 8, 5000])
+@pytest.mark.parametrize("which", ["q", "k", "v"])
+def test_the_longest_stride_is_the_documented_one(lib, which, tokens):
+    """(tokens + 512) * stride * 2 bytes below 4 GiB, for q, k and v: one step of 8 more is refused.  (What is let through is refused for
+    its alignment, which is looked at later: nothing is launched.)"""
+    import ctypes
+    most = (2 ** 32 - 1) // (2 * (tokens + 512)) // 8 * 8
+    cu = (ctypes.c_int32 * 2)(0, tokens)
+    odd = 0x10008                                              # never dereferenced
+    for stride, status in ((most, 9), (most + 8, 2)):
+        s = {n: stride if n == which else 512 for n in "qkv"}
+        assert lib.vfm_cattn_fwd(odd, s["q"], odd, s["k"], odd, s["v"], cu, cu, 1, tokens, tokens, 4, 2, 128, 0.1, odd, odd, None, 0, 0, None) == status
+        assert lib.vfm_cattn_bwd(odd, s["q"], odd, s["k"], odd, s["v"], odd, odd, odd, cu, cu, 1, tokens, tokens, 4, 2, 128, 0.1, odd, 512, odd, 256,
+                                 odd, 256, odd, 1 << 40, 0, None) == status
