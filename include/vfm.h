@@ -470,8 +470,10 @@ VFM_API int vfm_cattn_bwd(const void* q, int64_t q_stride, const void* k, int64_
  *   k_scales, v_scales  uint8 [n_pages][n_kv_heads][page_size][head_dim / 32]
  * A row (token, K/V head) is cut into blocks of 32 consecutive elements.  An element is an
  * E2M1 code (sign, 2 exponent bits, 1 mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6), two to a
- * byte, element 2b in the low half of byte b; a block's scale byte x in 1..254 stands for the
- * factor 2^(x - 127) (E8M0): value = code * factor.  vfm_kv4_append takes
+ * byte, element 2b in the low half of byte b; a block's scale byte x in 7..252 stands for the
+ * factor 2^(x - 127) (E8M0): value = code * factor, which bf16 holds exactly.  (A cache that
+ * something else has written keeps to that range too: beyond it values over- or underflow bf16, and an
+ * infinity at a place that a token does not see could reach its row.)  vfm_kv4_append takes
  *   e      = the largest integer with  max|x| * 2^e <= 6  over the block, limited to
  *            [-125, 120], 0 for an all-zero block;   scale byte = 127 - e
  *   code   = x * 2^e rounded to the nearest (ties to even, at most 6 in magnitude)

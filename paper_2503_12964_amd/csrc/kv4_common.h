@@ -4,7 +4,8 @@
 // exponent bits, one mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6), two to a byte, first element in the low half, and
 // one byte b per block for the factor 2^(b - 127).  A power-of-two factor makes every step but the rounding to a code
 // exact, and the conversion instructions of this chip take it as an operand: a row goes back to bf16 at one
-// instruction per two elements, products and all.  b = 255 marks a block that held a NaN or an infinity.
+// instruction per two elements, products and all.  b is 7 .. 252 (every code times the factor is a normal bf16); 255 marks a block that
+// held a NaN or an infinity.
 #pragma once
 
 #include "vfm_common.h"
