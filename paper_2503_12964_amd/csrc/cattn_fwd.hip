@@ -8,7 +8,8 @@
 // O^T += V^T P^T as it stands, S(u+1) and O += V(u-1) P(u-1) run under the softmax of unit u, the softmax reference moves only when
 // a unit's exponentials would grow too large, K and V in rings of four LDS slots.  What the causal order adds: a wavefront masks only the
 // units that reach past its first row's limit, computes none past its last row's (it keeps fetching its share and
-// meeting the barriers for the wavefronts behind it), and row tiles are handed out longest first.
+// meeting the barriers for the wavefronts behind it), and a sequence's row tiles are handed out longest first, the sequence with the
+// most keys first (the tiles of all sequences together are in no order).
 // Bound by the matrix pipe with the exponentials beside it: 12,007 tokens x 32/8 heads x 128 in 1,045 us, 1.13 PFLOP/s of the pairs that
 // are seen (a large library product on the same card: 1.33).
 #include "cattn_careful.h"
@@ -39,7 +40,7 @@ constexpr int kSgcValu = 0x002, kSgcMfma = 0x008, kSgcDsRead = 0x100;
 // Wavefronts per SIMD
 constexpr int fwd_waves(int D, int W) { return W == 1 ? 1 : W == 2 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2; }
 // In a cut call, which has a workgroup per CU: room for what the loop over tiles keeps (spilled otherwise: 2,000 tokens x 8/2 heads x 64
-// took 27 us, not 22).
+// took 27 us, not 22).  Eight wavefronts are two per SIMD in any case: 24 registers of the loop over tiles are spilled there.
 constexpr int split_waves(int D, int W) { return W == 4 ? (D == 64 ? 2 : 1) : fwd_waves(D, W); }
 
 // A wavefront's sums over keys [j0, j1) hold a NaN: they are formed again over the keys that each row sees, if those that

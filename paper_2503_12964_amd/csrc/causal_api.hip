@@ -56,8 +56,9 @@ int check_causal(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, int tota
   return st;
 }
 
-// Sequences of one run, longest key range first: a sequence's costliest tiles come first within it, so the grid begins with long
-// units and ends with short ones.  Sequences with neither queries nor keys are dropped.
+// Sequences of one run, longest key range first; a sequence's costliest tiles come first within it.  (Its short ones still come before
+// the next sequence's long ones: all tiles of a call in order of length would need a table of tiles.)  Sequences with neither
+// queries nor keys are dropped.
 void build_table(const int32_t* cu_q, const int32_t* cu_kv, int n_seqs, XSegTable* t) {
   int order[VFM_MAX_XSEQS];
   int n = 0;

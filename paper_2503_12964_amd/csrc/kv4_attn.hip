@@ -2,7 +2,7 @@
 //
 //     out_i = sum_j softmax_j(scale q_i . k_j) v_j,   j <= lens + t_i   (k_j, v_j: the values that the cache holds)
 //
-// Few rows against many keys: the cache is read once per row block and nothing else is big, so HBM bounds it (72 bytes of
+// Few rows against many keys: the cache is read once per row block and nothing else is big, so HBM bounds it (68 bytes of
 // K and of V per token and head at head_dim 128 against 4 * 128 operations a row).  What follows from that:
 //  - The cache's rows are read as they lie, 16 bytes of codes (32 elements) and their factor byte per lane.  The contraction of
 //    the score product may run in any order, so a lane's 32 consecutive elements of K are its operand of four
