@@ -897,19 +897,6 @@ struct Dq2Cfg {
   static constexpr int kChunksPerThread = kDqBC * kChunksPerRow / (kDq2Waves * 64);
 };
 
-// Sum over a lane's row of 16 lanes, in every lane: v + the value 8, then 4, 2, 1 lanes away (rotations).
-__device__ __forceinline__ float row16_sum(float v) {
-  auto add = [&](auto ror) {
-    constexpr int kRor = 0x120 + decltype(ror)::value;   // row_ror
-    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kRor, 0xf, 0xf, true));
-  };
-  add(IntC<8>{});
-  add(IntC<4>{});
-  add(IntC<2>{});
-  add(IntC<1>{});
-  return v;
-}
-
 // The work of one workgroup: query tile tq of sequence seq, one head.  STATS: form Delta and lse in log2
 // units of the tile's rows here, from `out` and `lse`, and leave them for the dK/dV pass (Delta of a sequence
 // with few keys is already in place).  The rows of dO are in LDS on their way into registers, so this costs the

@@ -37,19 +37,6 @@ __device__ __forceinline__ float few_delta(const f32x16& s, const f32x16& dp, fl
   return pair_sum(sum);
 }
 
-// Sum over a lane's row of 16 lanes, in every lane (rotations by 8, 4, 2, 1).
-__device__ __forceinline__ float row16_total(float v) {
-  auto add = [&](auto ror) {
-    constexpr int kRor = 0x120 + decltype(ror)::value;   // row_ror
-    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kRor, 0xf, 0xf, true));
-  };
-  add(IntC<8>{});
-  add(IntC<4>{});
-  add(IntC<2>{});
-  add(IntC<1>{});
-  return v;
-}
-
 // The sums of a wavefront's 32 rows over the 32-key blocks b0, b0 + step .. below key j1 hold a NaN: they are formed again over the
 // keys that each row sees, if those that it does not see may have made one.
 template <int D>
@@ -271,7 +258,7 @@ void cattn_dq2_kernel(const __bf16* __restrict__ q, const __bf16* __restrict__ k
       s[x] = 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[x] = __builtin_fmaf((float)orow[x][e], (float)d[e], s[x]);
-      s[x] = row16_total(s[x]);
+      s[x] = row16_sum(s[x]);
     }
 #pragma unroll
     for (int ib = 0; ib < 2; ++ib)

@@ -19,7 +19,6 @@
 namespace vfm {
 
 constexpr int kCRing = 4;               // LDS ring slots for K and for V
-constexpr float kCLog2e = 1.4426950408889634f;
 constexpr float kCLn2 = 0.6931471805599453f;
 constexpr float kCUnset = -3.0e38f;      // reference of a row that has seen no key
 constexpr float kCSafeSum = 256.0f;     // a unit's exponentials may sum to this before the reference moves

@@ -588,6 +588,19 @@ __device__ __forceinline__ void wait_vmcnt() {
 }
 template <int V>
 struct IntC { static constexpr int value = V; };
+
+// Sum over a lane's row of 16 lanes, in every lane: v + the value 8, then 4, 2, 1 lanes away (rotations).
+__device__ __forceinline__ float row16_sum(float v) {
+  auto add = [&](auto ror) {
+    constexpr int kRor = 0x120 + decltype(ror)::value;   // row_ror
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kRor, 0xf, 0xf, true));
+  };
+  add(IntC<8>{});
+  add(IntC<4>{});
+  add(IntC<2>{});
+  add(IntC<1>{});
+  return v;
+}
 // Marks a loaded operand as used here, so that the compiler waits for its global load at
 // this point (before the main loop) instead of keeping conservative vmcnt waits inside
 // the loop, where they would also wait for the direct-to-LDS loads in flight.
